@@ -17,9 +17,10 @@ DQ_OK = 0
 DQ_ERR_NULL, DQ_ERR_SHAPE, DQ_ERR_DTYPE, DQ_ERR_ALIGN, DQ_ERR_WORKSPACE, DQ_ERR_HIP, DQ_ERR_UNSUPPORTED = range(1, 8)
 DQ_F32, DQ_BF16 = 0, 1
 DQ_REDUCE_TOKEN_MEAN, DQ_REDUCE_SUM = 0, 1
-DQ_OBJ_WHIP, DQ_OBJ_VARIANCE, DQ_OBJ_KURTOSIS, DQ_OBJ_QUANT = 0, 1, 2, 3
+DQ_OBJ_WHIP, DQ_OBJ_VARIANCE, DQ_OBJ_KURTOSIS, DQ_OBJ_QUANT, DQ_OBJ_MXFP4, DQ_OBJ_MXFP8 = range(6)
+DQ_MXFP4, DQ_MXFP8 = 0, 1
 DQ_FLAG_SINGULAR, DQ_FLAG_NONFINITE, DQ_FLAG_ILLCOND_PANEL, DQ_FLAG_BAD_INDEX, DQ_FLAG_SYNC_TIMEOUT = 1, 2, 4, 8, 16
-DQ_K_GEMM_F32, DQ_K_GEMM_BF16, DQ_K_WHIP, DQ_K_PANEL, DQ_K_SMALL, DQ_K_COUNT = range(6)
+DQ_K_GEMM_F32, DQ_K_GEMM_BF16, DQ_K_WHIP, DQ_K_PANEL, DQ_K_SMALL, DQ_K_GEMM_MX, DQ_K_COUNT = range(7)
 DQ_OPT_ACCUM_PANELS, DQ_OPT_TALL_PANEL_MIN_ROWS, DQ_OPT_SINGLE_STREAM, DQ_OPT_FUSED_WHIP, DQ_OPT_HEADS_BATCHED, DQ_OPT_DEVICE_SYNC, DQ_OPT_SPLIT_GEMM, DQ_OPT_FUSED_PANEL, DQ_OPT_TWO_LEVEL_ROWS = range(9)
 DQ_MAX_N = 8192
 
@@ -57,6 +58,11 @@ SIGNATURES = {
     "dq_cayley_step": (_i, [_vp, _i, _i, _i, _vp, _i, _l, _vp, _l, _vp, _l, _f, _f, _f, _i, _f, _i, _vp]),
     "dq_gemm_f32": (_i, [_vp, _i, _i, _i, _f, _vp, _l, _i, _vp, _l, _i, _f, _vp, _l]),
     "dq_gemm_bf16": (_i, [_vp, _i, _i, _i, _vp, _l, _i, _vp, _l, _i, _vp, _l]),
+    "dq_mx_row_bytes": (_i, [_i, _i, _c.POINTER(_sz), _c.POINTER(_sz)]),
+    "dq_mx_quantize": (_i, [_vp, _i, _i, _vp, _i, _l, _i, _vp, _l, _vp, _l]),
+    "dq_mx_dequantize": (_i, [_vp, _i, _i, _i, _vp, _l, _vp, _l, _vp, _i, _l]),
+    "dq_mx_rms_norm": (_i, [_vp, _i, _i, _vp, _i, _l, _vp, _l, _vp, _l, _vp, _f, _i, _vp, _l, _vp, _l]),
+    "dq_gemm_mx": (_i, [_vp, _i, _i, _i, _i, _vp, _l, _vp, _l, _i, _vp, _l, _vp, _l, _vp, _i, _l]),
     "dq_profile_enable": (_i, [_vp, _c.c_uint]),
     "dq_profile_read": (_i, [_vp, _i, _c.POINTER(_c.c_double), _c.POINTER(_l), _c.POINTER(_c.c_double),
                              _c.POINTER(_c.c_double)]),
@@ -104,6 +110,15 @@ def workspace_bytes(b: int, n: int, T: int, x_dtype: int) -> int:
     if st != DQ_OK:
         raise DartQRError(st, "dq_workspace_bytes")
     return int(out.value)
+
+
+def dq_mx_row_bytes(fmt: int, n: int) -> tuple[int, int]:
+    """Bytes of codes and of scales of a row of n values."""
+    codes, scales = _sz(0), _sz(0)
+    st = load_library().dq_mx_row_bytes(fmt, n, ctypes.byref(codes), ctypes.byref(scales))
+    if st != DQ_OK:
+        raise DartQRError(st, "dq_mx_row_bytes")
+    return int(codes.value), int(scales.value)
 
 
 def _ptr(t):
@@ -304,6 +319,26 @@ class Context:
     def dq_gemm_bf16(self, M, N, K, A, ta, B, tb, C):
         self._check(self.lib.dq_gemm_bf16(self.h, M, N, K, _ptr(A), _ld(A), int(ta), _ptr(B), _ld(B), int(tb),
                                           _ptr(C), _ld(C)), "dq_gemm_bf16")
+
+    # ---- MX blocks (codes and scales: uint8 tensors whose rows hold dq_mx_row_bytes bytes)
+    def dq_mx_quantize(self, X, x_dtype, fmt, codes, scales):
+        T, n = X.shape
+        self._check(self.lib.dq_mx_quantize(self.h, T, n, _ptr(X), x_dtype, _ld(X), fmt, _ptr(codes), _ld(codes), _ptr(scales), _ld(scales)),
+                    "dq_mx_quantize")
+
+    def dq_mx_dequantize(self, fmt, codes, scales, Y, y_dtype):
+        T, n = Y.shape
+        self._check(self.lib.dq_mx_dequantize(self.h, T, n, fmt, _ptr(codes), _ld(codes), _ptr(scales), _ld(scales), _ptr(Y), y_dtype, _ld(Y)),
+                    "dq_mx_dequantize")
+
+    def dq_mx_rms_norm(self, X, x_dtype, residual, H, gain, eps, fmt, codes, scales):
+        T, n = X.shape
+        self._check(self.lib.dq_mx_rms_norm(self.h, T, n, _ptr(X), x_dtype, _ld(X), _ptr(residual), _ld(residual), _ptr(H), _ld(H), _ptr(gain),
+                                            eps, fmt, _ptr(codes), _ld(codes), _ptr(scales), _ld(scales)), "dq_mx_rms_norm")
+
+    def dq_gemm_mx(self, M, N, K, fa, A, A_scales, fb, B, B_scales, C, c_dtype):
+        self._check(self.lib.dq_gemm_mx(self.h, M, N, K, fa, _ptr(A), _ld(A), _ptr(A_scales), _ld(A_scales), fb, _ptr(B), _ld(B),
+                                        _ptr(B_scales), _ld(B_scales), _ptr(C), c_dtype, _ld(C)), "dq_gemm_mx")
 
     # ---- measurement
     def dq_profile_enable(self, mask: int):

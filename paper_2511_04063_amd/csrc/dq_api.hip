@@ -230,6 +230,39 @@ dq_status check_ws(dq_ctx* c, const Layout& L) {
     return DQ_OK;
 }
 
+bool known_objective(dq_objective o) { return (int)o >= DQ_OBJ_WHIP && (int)o <= DQ_OBJ_MXFP8; }
+
+// rows of MX blocks: n codes in whole blocks, and their scales in multiples of 16
+bool known_format(dq_mx_format f) { return f == DQ_MXFP4 || f == DQ_MXFP8; }
+long mx_code_bytes(dq_mx_format f, int n) { return (n + 31L) / 32 * (f == DQ_MXFP4 ? 16 : 32); }
+long mx_scale_bytes(int n) { return round_up((n + 31L) / 32, 16); }
+dq_status check_bytes(const void* p, long ld, long row) {
+    if (p == nullptr) return DQ_ERR_NULL;
+    if (ld < row) return DQ_ERR_SHAPE;
+    if (!aligned16(p) || (ld & 15) != 0) return DQ_ERR_ALIGN;
+    return DQ_OK;
+}
+dq_status check_mx(dq_mx_format f, int n, const void* codes, long ldc, const void* scales, long lds) {
+    if (!known_format(f)) return DQ_ERR_DTYPE;
+    const dq_status st = check_bytes(codes, ldc, mx_code_bytes(f, n));
+    return st != DQ_OK ? st : check_bytes(scales, lds, mx_scale_bytes(n));
+}
+
+// The context's device is the current one for the scope's lifetime.
+struct DeviceScope {
+    int before = -1;
+    bool ok = false;
+    explicit DeviceScope(int device) {
+        int now = -1;
+        if (hipGetDevice(&now) != hipSuccess) return;
+        if (now == device) { ok = true; return; }
+        if (hipSetDevice(device) != hipSuccess) return;
+        before = now;
+        ok = true;
+    }
+    ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
 #define DQ_TRY(expr)                      \
     do {                                  \
         const dq_status _s = (expr);      \
@@ -1951,7 +1984,7 @@ dq_status dq_objective_loss_grad(dq_ctx* c, dq_objective objective, int quant_bi
                                  long ldy, dq_reduce red, float* loss_dev, void* dY, dq_dtype dydt, long lddy) {
     if (objective == DQ_OBJ_WHIP) return dq_whip_loss_grad(c, b, T, n, Y, ldy, red, loss_dev, dY, dydt, lddy);
     if (c == nullptr || loss_dev == nullptr) return DQ_ERR_NULL;
-    if (objective != DQ_OBJ_VARIANCE && objective != DQ_OBJ_KURTOSIS && objective != DQ_OBJ_QUANT) return DQ_ERR_DTYPE;
+    if (!known_objective(objective)) return DQ_ERR_DTYPE;
     if (b < 0 || T < 1 || n < 1 || quant_bits < 1 || quant_bits > 16) return DQ_ERR_SHAPE;
     if (n > DQ_MAX_N) return DQ_ERR_UNSUPPORTED;
     if (red != DQ_REDUCE_TOKEN_MEAN && red != DQ_REDUCE_SUM) return DQ_ERR_DTYPE;
@@ -1979,9 +2012,7 @@ dq_status dq_objective_loss_grad(dq_ctx* c, dq_objective objective, int quant_bi
 
 dq_status dq_set_objective(dq_ctx* c, dq_objective objective, int quant_bits) {
     if (c == nullptr) return DQ_ERR_NULL;
-    if (objective != DQ_OBJ_WHIP && objective != DQ_OBJ_VARIANCE && objective != DQ_OBJ_KURTOSIS &&
-        objective != DQ_OBJ_QUANT)
-        return DQ_ERR_DTYPE;
+    if (!known_objective(objective)) return DQ_ERR_DTYPE;
     if (quant_bits < 1 || quant_bits > 16) return DQ_ERR_SHAPE;
     c->objective = objective;
     c->quant_bits = quant_bits;
@@ -2264,6 +2295,97 @@ dq_status dq_gemm_bf16(dq_ctx* c, int M, int N, int K, const void* A, long lda, 
     g.C = C; g.ldc = ldc; g.M = M; g.N = N; g.K = K;
     LaunchScope sc(&c->prof, c->stream, DQ_K_GEMM_BF16, 2.0 * M * (double)N * K, 0.0);
     DQ_HIP(launch_gemm_bf16(g, c->stream));
+    return DQ_OK;
+}
+
+dq_status dq_mx_row_bytes(dq_mx_format format, int n, size_t* codes, size_t* scales) {
+    if (codes == nullptr || scales == nullptr) return DQ_ERR_NULL;
+    if (n < 1) return DQ_ERR_SHAPE;
+    if (!known_format(format)) return DQ_ERR_DTYPE;
+    *codes = (size_t)mx_code_bytes(format, n);
+    *scales = (size_t)mx_scale_bytes(n);
+    return DQ_OK;
+}
+
+dq_status dq_mx_quantize(dq_ctx* c, int T, int n, const void* X, dq_dtype xdt, long ldx, dq_mx_format format, void* codes, long ldc, void* scales,
+                         long lds) {
+    if (c == nullptr) return DQ_ERR_NULL;
+    if (T < 0 || n < 1) return DQ_ERR_SHAPE;
+    if (T == 0) return DQ_OK;
+    DQ_TRY(check_x(X, xdt, ldx, n));
+    DQ_TRY(check_mx(format, n, codes, ldc, scales, lds));
+    if (c->ws == nullptr) return DQ_ERR_WORKSPACE;
+    const DeviceScope device(c->device);
+    if (!device.ok) return DQ_ERR_HIP;
+    const double esz = xdt == DQ_BF16 ? 2.0 : 4.0;
+    LaunchScope sc(&c->prof, c->stream, DQ_K_SMALL, 0.0, (double)T * (n * esz + mx_code_bytes(format, n) + mx_scale_bytes(n)));
+    DQ_HIP(launch_mx_quantize(X, xdt == DQ_BF16, ldx, T, n, format, static_cast<unsigned char*>(codes), ldc, static_cast<unsigned char*>(scales), lds,
+                              at<unsigned>(c, 0), c->stream));
+    return DQ_OK;
+}
+
+dq_status dq_mx_dequantize(dq_ctx* c, int T, int n, dq_mx_format format, const void* codes, long ldc, const void* scales, long lds, void* Y,
+                           dq_dtype ydt, long ldy) {
+    if (c == nullptr) return DQ_ERR_NULL;
+    if (T < 0 || n < 1) return DQ_ERR_SHAPE;
+    if (T == 0) return DQ_OK;
+    DQ_TRY(check_mx(format, n, codes, ldc, scales, lds));
+    DQ_TRY(check_x(Y, ydt, ldy, n));
+    const DeviceScope device(c->device);
+    if (!device.ok) return DQ_ERR_HIP;
+    const double esz = ydt == DQ_BF16 ? 2.0 : 4.0;
+    LaunchScope sc(&c->prof, c->stream, DQ_K_SMALL, 0.0, (double)T * (n * esz + mx_code_bytes(format, n) + mx_scale_bytes(n)));
+    DQ_HIP(launch_mx_dequantize(format, static_cast<const unsigned char*>(codes), ldc, static_cast<const unsigned char*>(scales), lds, T, n, Y,
+                                ydt == DQ_BF16, ldy, c->stream));
+    return DQ_OK;
+}
+
+dq_status dq_mx_rms_norm(dq_ctx* c, int T, int n, const void* X, dq_dtype xdt, long ldx, const void* residual, long ldr, void* H, long ldh,
+                         const float* gain, float eps, dq_mx_format format, void* codes, long ldc, void* scales, long lds) {
+    if (c == nullptr) return DQ_ERR_NULL;
+    if (T < 0) return DQ_ERR_SHAPE;
+    DQ_TRY(check_n(n));
+    if (!(eps >= 0.f) || eps > 3.0e38f) return DQ_ERR_SHAPE;
+    if (T == 0) return DQ_OK;
+    DQ_TRY(check_x(X, xdt, ldx, n));
+    if (residual != nullptr) DQ_TRY(check_x(residual, xdt, ldr, n));
+    if (H != nullptr) DQ_TRY(check_x(H, xdt, ldh, n));
+    // in place is row by row: the same rows, not others
+    if (H != nullptr && ((H == X && ldh != ldx) || (H == residual && ldh != ldr))) return DQ_ERR_SHAPE;
+    if (gain != nullptr && !aligned16(gain)) return DQ_ERR_ALIGN;
+    DQ_TRY(check_mx(format, n, codes, ldc, scales, lds));
+    if (c->ws == nullptr) return DQ_ERR_WORKSPACE;
+    const DeviceScope device(c->device);
+    if (!device.ok) return DQ_ERR_HIP;
+    MxNorm m;
+    m.X = X; m.ldx = ldx; m.res = residual; m.ldr = ldr; m.H = H; m.ldh = ldh; m.gain = gain; m.eps = eps;
+    m.T = T; m.n = n; m.x_is_bf16 = xdt == DQ_BF16; m.format = format;
+    m.codes = static_cast<unsigned char*>(codes); m.ldc = ldc; m.scales = static_cast<unsigned char*>(scales); m.lds = lds;
+    m.flags = at<unsigned>(c, 0);
+    const double esz = (xdt == DQ_BF16 ? 2.0 : 4.0) * (1 + (residual != nullptr) + (H != nullptr));
+    LaunchScope sc(&c->prof, c->stream, DQ_K_SMALL, 4.0 * T * (double)n, (double)T * (n * esz + mx_code_bytes(format, n) + mx_scale_bytes(n)));
+    DQ_HIP(launch_mx_rms_norm(m, c->stream));
+    return DQ_OK;
+}
+
+dq_status dq_gemm_mx(dq_ctx* c, int M, int N, int K, dq_mx_format fa, const void* A, long lda, const void* A_scales, long ldas, dq_mx_format fb,
+                     const void* B, long ldb, const void* B_scales, long ldbs, void* C, dq_dtype cdt, long ldc) {
+    if (c == nullptr) return DQ_ERR_NULL;
+    if (M < 0 || N < 0 || K < 1) return DQ_ERR_SHAPE;
+    if (!known_format(fa) || !known_format(fb)) return DQ_ERR_DTYPE;
+    if (M == 0 || N == 0) return DQ_OK;
+    DQ_TRY(check_mx(fa, K, A, lda, A_scales, ldas));
+    DQ_TRY(check_mx(fb, K, B, ldb, B_scales, ldbs));
+    DQ_TRY(check_x(C, cdt, ldc, N));
+    const DeviceScope device(c->device);
+    if (!device.ok) return DQ_ERR_HIP;
+    GemmMx g;
+    g.A = static_cast<const unsigned char*>(A); g.lda = lda; g.As = static_cast<const unsigned char*>(A_scales); g.ldas = ldas;
+    g.B = static_cast<const unsigned char*>(B); g.ldb = ldb; g.Bs = static_cast<const unsigned char*>(B_scales); g.ldbs = ldbs;
+    g.C = C; g.ldc = ldc; g.M = M; g.N = N; g.K = K; g.fa = fa; g.fb = fb; g.c_is_bf16 = cdt == DQ_BF16;
+    LaunchScope sc(&c->prof, c->stream, DQ_K_GEMM_MX, 2.0 * M * (double)N * K,
+                   (double)M * mx_code_bytes(fa, K) + (double)N * mx_code_bytes(fb, K) + (double)M * N * (g.c_is_bf16 ? 2.0 : 4.0));
+    DQ_HIP(launch_gemm_mx(g, c->stream));
     return DQ_OK;
 }
 

@@ -366,4 +366,32 @@ hipError_t launch_objective(int objective, int bits, const float* Y, long ldy, i
                             int dy_is_bf16, long lddy, double* partials, int grid, hipStream_t s, int batch = 1,
                             long stride_y = 0, long stride_dy = 0);
 
+// ---- microscaled (MX) blocks (see dq_mx.h) ------------------------------------------
+hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int n, int format, unsigned char* codes, long ldc, unsigned char* scales,
+                              long lds, unsigned* flags, hipStream_t s);
+hipError_t launch_mx_dequantize(int format, const unsigned char* codes, long ldc, const unsigned char* scales, long lds, int T, int n, void* Y,
+                                int y_is_bf16, long ldy, hipStream_t s);
+struct MxNorm {
+    const void* X = nullptr; long ldx = 0;
+    const void* res = nullptr; long ldr = 0;   // optional; added to X
+    void* H = nullptr; long ldh = 0;           // optional: X + res as the norm sees it; may be X or res
+    const float* gain = nullptr;               // optional
+    float eps = 0.f;
+    int T = 0, n = 0, x_is_bf16 = 0, format = 0;
+    unsigned char* codes = nullptr; long ldc = 0;
+    unsigned char* scales = nullptr; long lds = 0;
+    unsigned* flags = nullptr;
+};
+hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s);
+// as launch_objective; 16-byte aligned rows of Y and (8-byte in bf16) of dY
+hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
+                               int grid, hipStream_t s, int batch, long stride_y, long stride_dy);
+struct GemmMx {
+    const unsigned char* A = nullptr; long lda = 0; const unsigned char* As = nullptr; long ldas = 0;
+    const unsigned char* B = nullptr; long ldb = 0; const unsigned char* Bs = nullptr; long ldbs = 0;
+    void* C = nullptr; long ldc = 0;
+    int M = 0, N = 0, K = 0, fa = 0, fb = 0, c_is_bf16 = 0;
+};
+hipError_t launch_gemm_mx(const GemmMx& g, hipStream_t s);
+
 }  // namespace dq

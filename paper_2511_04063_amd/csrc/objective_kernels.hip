@@ -15,7 +15,7 @@ namespace {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int OBJ_VARIANCE = 1, OBJ_KURTOSIS = 2, OBJ_QUANT = 3;
+constexpr int OBJ_VARIANCE = 1, OBJ_KURTOSIS = 2, OBJ_QUANT = 3, OBJ_MXFP4 = 4, OBJ_MXFP8 = 5;
 
 __device__ __forceinline__ float wave_sum(float v) {
     v += lane_xor<1>(v); v += lane_xor<2>(v); v += lane_xor<4>(v);
@@ -366,6 +366,10 @@ hipError_t launch_objective(int objective, int bits, const float* Y, long ldy, i
         case OBJ_QUANT:
             return launch_rows_shape<OBJ_QUANT>(Y, ldy, T, n, scale, levels, dY, dy_is_bf16, lddy, partials, grid,
                                                 batch, stride_y, stride_dy, s);
+        case OBJ_MXFP4:
+        case OBJ_MXFP8:
+            return launch_mx_objective(objective == OBJ_MXFP4 ? DQ_MXFP4 : DQ_MXFP8, Y, ldy, T, n, scale, dY, dy_is_bf16, lddy,
+                                       partials, grid, s, batch, stride_y, stride_dy);
         default: return hipErrorInvalidValue;
     }
 }
