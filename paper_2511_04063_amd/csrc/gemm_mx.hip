@@ -17,6 +17,7 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // operand format as the instruction counts it
@@ -155,9 +156,335 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g) {
     }
 }
 
+// ---- tiles through LDS: a workgroup of 2 x 2 wavefronts makes 64 MI x 64 NI of C, a wavefront 32 MI x 32 NI of it in 32 x 32 x 64 instructions
+// (lane l: row l % 32, block l / 32; 8-bit operands k = 16 g .. and k = 32 + 16 g .. for g = l / 32).
+//
+// The reduction goes in stages of 128.  kStages of them are on their way or in LDS; a lane's 16 bytes travel from memory into LDS without passing
+// registers.  What a wavefront waits for, in stage i: its own parts of stage i + 1, with kStages - 2 later stages still travelling, then a barrier;
+// behind it stage i + 1 is complete in LDS, and every wavefront has read the last of stage i, whose place the parts of stage i + kStages take.
+// The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for four stages, the same way: ordered
+// behind the transfers of stage i + kStages and in front of those of stage i + kStages + 1, they have arrived three stages later in any case.
+//
+// LDS holds rows of 64 (4-bit) or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
+// different banks, and so do sixteen.
+template <int F> constexpr int kChunks = kStepBytes<F> / 16;
+template <int F>
+__device__ __forceinline__ int swizzle(int row) {
+    const int b0 = row & 1, b1 = (row >> 1) & 1, b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
+    if constexpr (F == DQ_MXFP4) return (b1 ^ b3) | (b2 << 1);
+    else return (b0 ^ b3) | (b1 << 1) | (b2 << 2);
+}
+
+// 16 bytes a lane from base + offset to LDS at `to` + 16 lane; not waited for.  (M0 is a register that the compiler sets itself before each use.)
+__device__ __forceinline__ void to_lds(const unsigned char* base, unsigned offset, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void to_lds(const unsigned char* from, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+// all but the last N of this wavefront's transfers have arrived, its LDS reads are done, and every wavefront has come as far
+template <int N>
+__device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int FA, int FB, int MI, int NI>
+struct TileShape {
+    static constexpr int TM = 64 * MI, TN = 64 * NI;
+    static constexpr int RA = kStepBytes<FA>, RB = kStepBytes<FB>;       // bytes of a row in a stage
+    static constexpr int PA = TM * RA / 4096, PB = TN * RB / 4096;       // transfers of 16 bytes a thread and stage
+    static constexpr int kStageBytes = TM * RA + TN * RB;
+    static constexpr int kScaleBytes = (TM + TN) * 16;
+    static constexpr int kStages = 4 * kStageBytes + kScaleBytes <= 160 * 1024 ? 4 : 3 * kStageBytes + kScaleBytes <= 160 * 1024 ? 3 : 2;
+    static constexpr int kLds = kStages * kStageBytes + kScaleBytes;
+};
+
+template <int FA, int FB, class OUT, int MI, int NI>
+__global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
+    using S = TileShape<FA, FB, MI, NI>;
+    constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
+    constexpr int P = S::PA + S::PB, NST = S::kStages;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLds];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 31, q = lane >> 5;
+
+    // XCD-aware tile order (see gemm_f32.hip): the workgroups resident on an XCD form a block of tiles 8 high
+    const int nt = tiles_m * tiles_n;
+    const int bid = blockIdx.x;
+    const int q8 = nt >> 3, r8 = nt & 7;
+    const int xcd = bid & 7;
+    const int pid = xcd * q8 + (xcd < r8 ? xcd : r8) + (bid >> 3);
+    const int group = 8 * tiles_n;
+    const int first_m = pid / group * 8;
+    const int gsz = (tiles_m - first_m) < 8 ? (tiles_m - first_m) : 8;
+    const int m0 = (first_m + (pid % group) % gsz) * S::TM, n0 = (pid % group) / gsz * S::TN;
+
+    const int nb = (int)((g.K + 31L) / 32), stages = (nb + 3) / 4;
+    const unsigned smem_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
+    constexpr int kScalesAt = NST * S::kStageBytes;
+
+    // this thread's transfers: row and chunk in a tile, as an offset from the tile's first row
+    const unsigned char* const baseA = g.A + (long)m0 * g.lda;
+    const unsigned char* const baseB = g.B + (long)n0 * g.ldb;
+    unsigned offA[S::PA], offB[S::PB];
+    int chunkA, chunkB;          // the same for all of a thread's rows, which are 16 or a multiple of it apart
+    {
+        constexpr int rows = 256 / kChunks<FA>;
+        const int at = tid / kChunks<FA>;
+        chunkA = (tid % kChunks<FA>) ^ swizzle<FA>(at);
+#pragma unroll
+        for (int p = 0; p < S::PA; ++p) {
+            const int row = m0 + p * rows + at < g.M ? p * rows + at : g.M - 1 - m0;
+            offA[p] = (unsigned)((long)row * g.lda) + 16u * chunkA;
+        }
+    }
+    {
+        constexpr int rows = 256 / kChunks<FB>;
+        const int at = tid / kChunks<FB>;
+        chunkB = (tid % kChunks<FB>) ^ swizzle<FB>(at);
+#pragma unroll
+        for (int p = 0; p < S::PB; ++p) {
+            const int row = n0 + p * rows + at < g.N ? p * rows + at : g.N - 1 - n0;
+            offB[p] = (unsigned)((long)row * g.ldb) + 16u * chunkB;
+        }
+    }
+    constexpr int SP = (S::TM + S::TN + 255) / 256;
+    const unsigned char* scale_row[SP];
+#pragma unroll
+    for (int p = 0; p < SP; ++p) {
+        const int i = p * 256 + tid;
+        if (i < S::TM) {
+            const int row = m0 + i < g.M ? m0 + i : g.M - 1;
+            scale_row[p] = g.As + (long)row * g.ldas;
+        } else {
+            const int row = n0 + i - S::TM < g.N ? n0 + i - S::TM : g.N - 1;
+            scale_row[p] = g.Bs + (long)row * g.ldbs;
+        }
+    }
+    // Piece p of a stage into `place` (a place holds A's rows, then B's).  In the last stage, which stands in for all behind it too, a chunk of a
+    // block that the row does not have is replaced by the row's first one of the stage: its scale counts as 2^-127 in both operands, which makes nothing
+    // of any number, and a NaN in it has made the row NaN before.
+    const unsigned backA = 4 * (stages - 1) + chunkA / (kChunks<FA> / 4) < nb ? 0u : 16u * chunkA;
+    const unsigned backB = 4 * (stages - 1) + chunkB / (kChunks<FB> / 4) < nb ? 0u : 16u * chunkB;
+    struct Source { const unsigned char *a, *b; unsigned back_a, back_b; };
+    auto source = [&](int t) {
+        const bool last = t >= stages - 1;
+        t = last ? stages - 1 : t;
+        return Source{baseA + (long)t * S::RA, baseB + (long)t * S::RB, last ? backA : 0u, last ? backB : 0u};
+    };
+    auto fetch = [&](const Source& f, int p, int place) {
+        const bool a = p < S::PA;
+        const int pp = a ? p : p - S::PA;
+        const unsigned to = smem_at + place * S::kStageBytes + (a ? 0 : S::TM * S::RA) + pp * 4096 + wave * 1024;
+        to_lds(a ? f.a : f.b, a ? offA[a ? pp : 0] - f.back_a : offB[a ? 0 : pp] - f.back_b, to);
+    };
+    auto fetch_scales = [&](int chunk) {
+        chunk = 4 * chunk < stages ? chunk : (stages - 1) / 4;
+#pragma unroll
+        for (int p = 0; p < SP; ++p)
+            if (S::TM + S::TN >= 256 || wave * 64 < S::TM + S::TN)
+                to_lds(scale_row[p] + 16L * chunk, smem_at + kScalesAt + p * 4096 + wave * 1024);
+    };
+
+    const int wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NI;
+    const int rowA = (wm + r) * S::RA, rowB = S::TM * S::RA + (wn + r) * S::RB;
+    const int swA = swizzle<FA>(r), swB = swizzle<FB>(r);
+
+    Codes<FA> fa[2][MI];
+    Codes<FB> fb[2][NI];
+    // fragment k (A's, then B's) of step u of the stage at `place`
+    auto read = [&](auto& c, int at, int sw, auto fc, int u) {
+        constexpr int F = decltype(fc)::value;
+        const unsigned char* row = smem + at;
+        if constexpr (F == DQ_MXFP4) {
+            c.a = *reinterpret_cast<const i32x4*>(row + 16 * ((2 * u + q) ^ sw));
+        } else {
+            c.a = *reinterpret_cast<const i32x4*>(row + 16 * ((EXACT ? 4 * u + 2 * q : 4 * u + q) ^ sw));
+            c.b = *reinterpret_cast<const i32x4*>(row + 16 * ((EXACT ? 4 * u + 2 * q + 1 : 4 * u + 2 + q) ^ sw));
+        }
+    };
+    auto read_fragment = [&](int k, int set, int u, int place) {
+        if (k < MI) read(fa[set][k], place * S::kStageBytes + rowA + 32 * k * S::RA, swA, std::integral_constant<int, FA>{}, u);
+        else read(fb[set][k - MI], place * S::kStageBytes + rowB + 32 * (k - MI) * S::RB, swB, std::integral_constant<int, FB>{}, u);
+    };
+
+    // Scales of 512 of the reduction.  Rows i and i + 1 of fragments: the lanes of the lower half read 16 bytes of a row of fragment i, those of
+    // the upper half of fragment i + 1; bytes of even blocks and of odd ones are put together, and the halves exchanged, so that byte t of
+    // word pair sc[i] is, in each lane, the scale of its block in step t.
+    constexpr int FR = MI + NI;
+    i32x4 raw[(FR + 1) / 2];
+    int sc[FR][2];
+    auto frag_row = [&](int k) { return k < MI ? wm + 32 * k : S::TM + wn + 32 * (k - MI); };
+    auto read_scales = [&]() {
+#pragma unroll
+        for (int k = 0; k < FR; k += 2) {
+            const int row = q == 0 ? frag_row(k) : frag_row(k + 1 < FR ? k + 1 : k);
+            raw[k / 2] = *reinterpret_cast<const i32x4*>(smem + kScalesAt + 16 * (row + r));
+        }
+    };
+    auto place_scales = [&](int chunk) {
+        unsigned keep[4];            // what lies behind the row's last scale may be anything
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int have = nb - 16 * chunk - 4 * w;
+            keep[w] = have >= 4 ? ~0u : have <= 0 ? 0u : (1u << (8 * have)) - 1u;
+        }
+#pragma unroll
+        for (int k = 0; k < FR; k += 2) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const unsigned lo = (unsigned)raw[k / 2][2 * w] & keep[2 * w], hi = (unsigned)raw[k / 2][2 * w + 1] & keep[2 * w + 1];
+                const unsigned even = __builtin_amdgcn_perm(hi, lo, 0x06040200u), odd = __builtin_amdgcn_perm(hi, lo, 0x07050301u);
+                const auto x = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+                sc[k][w] = (int)x[0];
+                if (k + 1 < FR) sc[k + 1 < FR ? k + 1 : k][w] = (int)x[1];
+            }
+        }
+    };
+
+    f32x16 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    // Step T of the eight of a piece of 512.  In the second step of a stage the next stage's first fragments are read and the place of this
+    // one is filled again.  No branches: the instructions stay where they are written, each transfer and read behind a multiplication of its own.
+    int place = 0;
+    auto step = [&](auto tc, int stage) {
+        constexpr int T = decltype(tc)::value, u = T & 1;
+        int next_place = place;
+        Source from;
+        if constexpr (u == 1) {
+            arrived<(NST - 2) * P>();
+            next_place = place + 1 == NST ? 0 : place + 1;
+            from = source(stage + NST);
+            if constexpr (T == 7) read_scales();
+        }
+        constexpr int SLOTS = MI * NI, READS = (FR + SLOTS - 1) / SLOTS, PULLS = (P + SLOTS - 1) / SLOTS;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int i = s / NI, j = (i & 1) ? NI - 1 - s % NI : s % NI;
+            if constexpr (EXACT) {
+                const unsigned ea = ((unsigned)sc[i][T / 4] >> (8 * (T & 3))) & 255u, eb = ((unsigned)sc[MI + j][T / 4] >> (8 * (T & 3))) & 255u;
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 0>(fb[u][j], eb), values8<FA, 0>(fa[u][i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 1>(fb[u][j], eb), values8<FA, 1>(fa[u][i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 2>(fb[u][j], eb), values8<FA, 2>(fa[u][i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 3>(fb[u][j], eb), values8<FA, 3>(fa[u][i], ea), acc[i][j], 0, 0, 0);
+            } else {
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(fb[u][j]), operand<FA>(fa[u][i]), acc[i][j], kMfmaFormat<FB>,
+                                                                            kMfmaFormat<FA>, T & 3, sc[MI + j][T / 4], T & 3, sc[i][T / 4]);
+            }
+#pragma unroll
+            for (int k = s * READS; k < (s + 1) * READS; ++k)
+                if (k < FR) read_fragment(k, 1 - u, 1 - u, next_place);
+            if constexpr (u == 1) {
+#pragma unroll
+                for (int k = s * PULLS; k < (s + 1) * PULLS; ++k)
+                    if (k < P) fetch(from, k, place);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (T == 1) fetch_scales(stage / 4 + 1);
+        if constexpr (u == 1) place = next_place;
+        if constexpr (T == 7) place_scales(stage / 4 + 1);
+    };
+
+    fetch_scales(0);
+#pragma unroll
+    for (int t = 0; t < NST; ++t) {
+        const Source from = source(t);
+#pragma unroll
+        for (int p = 0; p < P; ++p) fetch(from, p, t);
+    }
+    arrived<(NST - 1) * P>();
+    read_scales();
+#pragma unroll
+    for (int k = 0; k < FR; ++k) read_fragment(k, 0, 0, 0);
+    place_scales(0);
+    for (int stage = 0; stage < stages; stage += 4) {
+        step(std::integral_constant<int, 0>{}, stage);
+        step(std::integral_constant<int, 1>{}, stage);
+        step(std::integral_constant<int, 2>{}, stage + 1);
+        step(std::integral_constant<int, 3>{}, stage + 1);
+        step(std::integral_constant<int, 4>{}, stage + 2);
+        step(std::integral_constant<int, 5>{}, stage + 2);
+        step(std::integral_constant<int, 6>{}, stage + 3);
+        step(std::integral_constant<int, 7>{}, stage + 3);
+    }
+    arrived<0>();        // nothing may still be on its way into LDS when the workgroup ends
+
+    // register 4 x + y of a lane holds C[m = r][n = 8 x + 4 q + y]; lanes of the two halves exchange groups of four, so that each writes eight
+    // columns in a row: lower half 16 x .., upper half 16 x + 8 ..
+    OUT* C = static_cast<OUT*>(g.C);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int m = m0 + wm + 32 * i + r;
+        OUT* row = C + (long)m * g.ldc;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int n = n0 + wn + 32 * j + 16 * x + 8 * q;
+                unsigned w[8];
+                constexpr int W = sizeof(OUT) == 4 ? 4 : 2;       // words of four values
+                if constexpr (sizeof(OUT) == 4) {
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) w[v] = __float_as_uint(acc[i][j][8 * x + v]);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const mx_f32x2 pair = {acc[i][j][8 * x + 2 * v], acc[i][j][8 * x + 2 * v + 1]};
+                        w[v] = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, mx_bf16x2));
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < W; ++v) {
+                    const auto e = __builtin_amdgcn_permlane32_swap(w[v], w[v + W], false, false);
+                    w[v] = e[0];
+                    w[v + W] = e[1];
+                }
+                if (m >= g.M || n >= g.N) continue;
+                if (n + 8 <= g.N) {
+                    *reinterpret_cast<uint4*>(row + n) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<uint4*>(row + n + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 7; ++v)
+                        if (n + v < g.N) {
+                            if constexpr (sizeof(OUT) == 4) row[n + v] = __uint_as_float(w[v]);
+                            else row[n + v] = (bf16_t)(v & 1 ? w[v / 2] >> 16 : w[v / 2] & 0xffffu);
+                        }
+                }
+            }
+        }
+    }
+}
+
+template <int FA, int FB, class OUT, int MI, int NI>
+hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
+    using S = TileShape<FA, FB, MI, NI>;
+    const long tm = (g.M + (long)S::TM - 1) / S::TM, tn = (g.N + (long)S::TN - 1) / S::TN;
+    if (tm * tn > 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemm_mx_tile_kernel<FA, FB, OUT, MI, NI>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, g, (int)tm, (int)tn);
+    return hipGetLastError();
+}
+
 template <int FA, int FB, class OUT>
 hipError_t launch_types(const GemmMx& g, hipStream_t s) {
     const unsigned gx = (unsigned)((g.N + 15L) / 16);
+    // the tiles address 256 rows of codes by 32-bit offsets
+    const bool near_rows = g.lda < (1L << 23) && g.ldb < (1L << 23);
+    if (near_rows && g.M > 64) {
+        const long t256 = ((g.M + 255L) / 256) * ((g.N + 255L) / 256), t128 = ((g.M + 127L) / 128) * ((g.N + 127L) / 128);
+        constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
+        if constexpr (!exact)
+            if (t256 >= 192) return launch_tile<FA, FB, OUT, 4, 4>(g, s);
+        if (t128 >= 192) return launch_tile<FA, FB, OUT, 2, 2>(g, s);
+        return launch_tile<FA, FB, OUT, 1, 1>(g, s);
+    }
     if (g.M <= 16) hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 1>), dim3(gx, 1), dim3(512), 0, s, g);
     else hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 4>), dim3(gx, (unsigned)((g.M + 63L) / 64)), dim3(512), 0, s, g);
     return hipGetLastError();
