@@ -159,19 +159,18 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g) {
 // ---- tiles through LDS: a workgroup of 2 x 2 wavefronts makes 64 MI x 64 NI of C, a wavefront 32 MI x 32 NI of it in 32 x 32 x 64 instructions
 // (lane l: row l % 32, block l / 32; 8-bit operands k = 16 g .. and k = 32 + 16 g .. for g = l / 32).
 //
-// The reduction goes in stages of 128.  kStages of them are on their way or in LDS; a lane's 16 bytes travel from memory into LDS without passing
+// The reduction goes in stages of 128, or of 64 where both operands have 8 bits.  kStages of them are on their way or in LDS; a lane's 16 bytes travel from memory into LDS without passing
 // registers.  What a wavefront waits for, in stage i: its own parts of stage i + 1, with kStages - 2 later stages still travelling, then a barrier;
 // behind it stage i + 1 is complete in LDS, and every wavefront has read the last of stage i, whose place the parts of stage i + kStages take.
-// The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for four stages, the same way: ordered
-// behind the transfers of stage i + kStages and in front of those of stage i + kStages + 1, they have arrived three stages later in any case.
+// The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for 512 of the reduction, the same
+// way; by the last step of the 512 before, at least kStages - 2 later stages have been sent for behind them, so that they have arrived.
 //
-// LDS holds rows of 64 (4-bit) or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
+// LDS holds rows of 64 or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
 // different banks, and so do sixteen.
-template <int F> constexpr int kChunks = kStepBytes<F> / 16;
-template <int F>
+template <int CHUNKS>
 __device__ __forceinline__ int swizzle(int row) {
     const int b0 = row & 1, b1 = (row >> 1) & 1, b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
-    if constexpr (F == DQ_MXFP4) return (b1 ^ b3) | (b2 << 1);
+    if constexpr (CHUNKS == 4) return (b1 ^ b3) | (b2 << 1);
     else return (b0 ^ b3) | (b1 << 1) | (b2 << 2);
 }
 
@@ -191,19 +190,22 @@ __device__ __forceinline__ void arrived() {
 template <int FA, int FB, int MI, int NI>
 struct TileShape {
     static constexpr int TM = 64 * MI, TN = 64 * NI;
-    static constexpr int RA = kStepBytes<FA>, RB = kStepBytes<FB>;       // bytes of a row in a stage
+    static constexpr int SUB = FA == DQ_MXFP8 && FB == DQ_MXFP8 ? 1 : 2;              // steps of 64 in a stage
+    static constexpr int RA = kStepBytes<FA> / 2 * SUB, RB = kStepBytes<FB> / 2 * SUB;   // bytes of a row in a stage
+    static constexpr int CA = RA / 16, CB = RB / 16;                     // chunks
     static constexpr int PA = TM * RA / 4096, PB = TN * RB / 4096;       // transfers of 16 bytes a thread and stage
     static constexpr int kStageBytes = TM * RA + TN * RB;
     static constexpr int kScaleBytes = (TM + TN) * 16;
-    static constexpr int kStages = 4 * kStageBytes + kScaleBytes <= 160 * 1024 ? 4 : 3 * kStageBytes + kScaleBytes <= 160 * 1024 ? 3 : 2;
+    static constexpr int kStages = 4 * kStageBytes + kScaleBytes <= 160 * 1024 ? 4 : 3;
     static constexpr int kLds = kStages * kStageBytes + kScaleBytes;
+    static_assert(kLds <= 160 * 1024, "stages have to fit LDS");
 };
 
 template <int FA, int FB, class OUT, int MI, int NI>
 __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
     using S = TileShape<FA, FB, MI, NI>;
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
-    constexpr int P = S::PA + S::PB, NST = S::kStages;
+    constexpr int P = S::PA + S::PB, NST = S::kStages, SUB = S::SUB, BLOCKS = 2 * SUB;      // blocks of a row in a stage
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, q = lane >> 5;
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     const int gsz = (tiles_m - first_m) < 8 ? (tiles_m - first_m) : 8;
     const int m0 = (first_m + (pid % group) % gsz) * S::TM, n0 = (pid % group) / gsz * S::TN;
 
-    const int nb = (int)((g.K + 31L) / 32), stages = (nb + 3) / 4;
+    const int nb = (int)((g.K + 31L) / 32), stages = (nb + BLOCKS - 1) / BLOCKS;
     const unsigned smem_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
     constexpr int kScalesAt = NST * S::kStageBytes;
 
@@ -229,9 +231,9 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     unsigned offA[S::PA], offB[S::PB];
     int chunkA, chunkB;          // the same for all of a thread's rows, which are 16 or a multiple of it apart
     {
-        constexpr int rows = 256 / kChunks<FA>;
-        const int at = tid / kChunks<FA>;
-        chunkA = (tid % kChunks<FA>) ^ swizzle<FA>(at);
+        constexpr int rows = 256 / S::CA;
+        const int at = tid / S::CA;
+        chunkA = (tid % S::CA) ^ swizzle<S::CA>(at);
 #pragma unroll
         for (int p = 0; p < S::PA; ++p) {
             const int row = m0 + p * rows + at < g.M ? p * rows + at : g.M - 1 - m0;
@@ -239,9 +241,9 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
         }
     }
     {
-        constexpr int rows = 256 / kChunks<FB>;
-        const int at = tid / kChunks<FB>;
-        chunkB = (tid % kChunks<FB>) ^ swizzle<FB>(at);
+        constexpr int rows = 256 / S::CB;
+        const int at = tid / S::CB;
+        chunkB = (tid % S::CB) ^ swizzle<S::CB>(at);
 #pragma unroll
         for (int p = 0; p < S::PB; ++p) {
             const int row = n0 + p * rows + at < g.N ? p * rows + at : g.N - 1 - n0;
@@ -264,8 +266,8 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     // Piece p of a stage into `place` (a place holds A's rows, then B's).  In the last stage, which stands in for all behind it too, a chunk of a
     // block that the row does not have is replaced by the row's first one of the stage: its scale counts as 2^-127 in both operands, which makes nothing
     // of any number, and a NaN in it has made the row NaN before.
-    const unsigned backA = 4 * (stages - 1) + chunkA / (kChunks<FA> / 4) < nb ? 0u : 16u * chunkA;
-    const unsigned backB = 4 * (stages - 1) + chunkB / (kChunks<FB> / 4) < nb ? 0u : 16u * chunkB;
+    const unsigned backA = BLOCKS * (stages - 1) + chunkA / (S::CA / BLOCKS) < nb ? 0u : 16u * chunkA;
+    const unsigned backB = BLOCKS * (stages - 1) + chunkB / (S::CB / BLOCKS) < nb ? 0u : 16u * chunkB;
     struct Source { const unsigned char *a, *b; unsigned back_a, back_b; };
     auto source = [&](int t) {
         const bool last = t >= stages - 1;
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
         to_lds(a ? f.a : f.b, a ? offA[a ? pp : 0] - f.back_a : offB[a ? 0 : pp] - f.back_b, to);
     };
     auto fetch_scales = [&](int chunk) {
-        chunk = 4 * chunk < stages ? chunk : (stages - 1) / 4;
+        chunk = 16 * chunk < nb ? chunk : (nb - 1) / 16;
 #pragma unroll
         for (int p = 0; p < SP; ++p)
             if (S::TM + S::TN >= 256 || wave * 64 < S::TM + S::TN)
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
 
     const int wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NI;
     const int rowA = (wm + r) * S::RA, rowB = S::TM * S::RA + (wn + r) * S::RB;
-    const int swA = swizzle<FA>(r), swB = swizzle<FB>(r);
+    const int swA = swizzle<S::CA>(r), swB = swizzle<S::CB>(r);
 
     Codes<FA> fa[2][MI];
     Codes<FB> fb[2][NI];
@@ -350,20 +352,24 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-    // Step T of the eight of a piece of 512.  In the second step of a stage the next stage's first fragments are read and the place of this
-    // one is filled again.  No branches: the instructions stay where they are written, each transfer and read behind a multiplication of its own.
+    // Step T of the eight of a piece of 512.  From the last step of a stage on its place is filled again (of two steps a stage: half of it there,
+    // half in the first step of the next); that step also reads the next stage's first fragments.  No branches: the instructions stay where they are written, each transfer and read behind a multiplication of its own.
+    constexpr int H = SUB == 1 ? P : P / 2;
+    auto before = [](int x) { return x == 0 ? NST - 1 : x - 1; };
     int place = 0;
+    Source from = source(NST - 1);
     auto step = [&](auto tc, int stage) {
         constexpr int T = decltype(tc)::value, u = T & 1;
+        constexpr bool last = T % SUB == SUB - 1;
         int next_place = place;
-        Source from;
-        if constexpr (u == 1) {
+        if constexpr (last) {
             arrived<(NST - 2) * P>();
             next_place = place + 1 == NST ? 0 : place + 1;
             from = source(stage + NST);
             if constexpr (T == 7) read_scales();
         }
-        constexpr int SLOTS = MI * NI, READS = (FR + SLOTS - 1) / SLOTS, PULLS = (P + SLOTS - 1) / SLOTS;
+        constexpr int SLOTS = MI * NI, READS = (FR + SLOTS - 1) / SLOTS;
+        constexpr int first = last ? 0 : H, count = last ? H : P - H;            // transfers of this step
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
             const int i = s / NI, j = (i & 1) ? NI - 1 - s % NI : s % NI;
@@ -379,40 +385,38 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
             }
 #pragma unroll
             for (int k = s * READS; k < (s + 1) * READS; ++k)
-                if (k < FR) read_fragment(k, 1 - u, 1 - u, next_place);
-            if constexpr (u == 1) {
+                if (k < FR) read_fragment(k, 1 - u, last ? 0 : 1, next_place);
+            // evenly over the step: a wavefront waits where the four send more than the memory path takes in
 #pragma unroll
-                for (int k = s * PULLS; k < (s + 1) * PULLS; ++k)
-                    if (k < P) fetch(from, k, place);
-            }
+            for (int k = count * s / SLOTS; k < count * (s + 1) / SLOTS; ++k) fetch(from, first + k, last ? place : before(place));
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (T == 1) fetch_scales(stage / 4 + 1);
-        if constexpr (u == 1) place = next_place;
-        if constexpr (T == 7) place_scales(stage / 4 + 1);
+        if constexpr (T == 1) fetch_scales(stage * SUB / 8 + 1);
+        if constexpr (last) place = next_place;
+        if constexpr (T == 7) place_scales(stage * SUB / 8 + 1);
     };
 
     fetch_scales(0);
 #pragma unroll
     for (int t = 0; t < NST; ++t) {
-        const Source from = source(t);
+        const Source first = source(t);
 #pragma unroll
-        for (int p = 0; p < P; ++p) fetch(from, p, t);
+        for (int p = 0; p < (t + 1 < NST ? P : H); ++p) fetch(first, p, t);
     }
-    arrived<(NST - 1) * P>();
+    arrived<(NST - 2) * P + H>();
     read_scales();
 #pragma unroll
     for (int k = 0; k < FR; ++k) read_fragment(k, 0, 0, 0);
     place_scales(0);
-    for (int stage = 0; stage < stages; stage += 4) {
+    for (int stage = 0; stage < stages; stage += 8 / SUB) {
         step(std::integral_constant<int, 0>{}, stage);
-        step(std::integral_constant<int, 1>{}, stage);
-        step(std::integral_constant<int, 2>{}, stage + 1);
-        step(std::integral_constant<int, 3>{}, stage + 1);
-        step(std::integral_constant<int, 4>{}, stage + 2);
-        step(std::integral_constant<int, 5>{}, stage + 2);
-        step(std::integral_constant<int, 6>{}, stage + 3);
-        step(std::integral_constant<int, 7>{}, stage + 3);
+        step(std::integral_constant<int, 1>{}, stage + 1 / SUB);
+        step(std::integral_constant<int, 2>{}, stage + 2 / SUB);
+        step(std::integral_constant<int, 3>{}, stage + 3 / SUB);
+        step(std::integral_constant<int, 4>{}, stage + 4 / SUB);
+        step(std::integral_constant<int, 5>{}, stage + 5 / SUB);
+        step(std::integral_constant<int, 6>{}, stage + 6 / SUB);
+        step(std::integral_constant<int, 7>{}, stage + 7 / SUB);
     }
     arrived<0>();        // nothing may still be on its way into LDS when the workgroup ends
 
