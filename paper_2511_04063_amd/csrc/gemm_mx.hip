@@ -159,14 +159,15 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g) {
 // ---- tiles through LDS: a workgroup of 2 x 2 wavefronts makes 64 MI x 64 NI of C, a wavefront 32 MI x 32 NI of it in 32 x 32 x 64 instructions
 // (lane l: row l % 32, block l / 32; 8-bit operands k = 16 g .. and k = 32 + 16 g .. for g = l / 32).
 //
-// The reduction goes in stages of 128, or of 64 where both operands have 8 bits.  kStages of them are on their way or in LDS; a lane's 16 bytes travel from memory into LDS without passing
-// registers.  What a wavefront waits for, in stage i: its own parts of stage i + 1, with kStages - 2 later stages still travelling, then a barrier;
-// behind it stage i + 1 is complete in LDS, and every wavefront has read the last of stage i, whose place the parts of stage i + kStages take.
-// The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for 512 of the reduction, the same
-// way; by the last step of the 512 before, at least kStages - 2 later stages have been sent for behind them, so that they have arrived.
+// The reduction goes in stages of 128 (of 256 where both operands have 4 bits: rows of 128 bytes, whole cache lines; with half of one a transfer the
+// requests doubled, and the path to memory was busy 77 % of the time instead of 54).  kStages of them are on their way or in LDS; a lane's 16 bytes
+// travel from memory into LDS without passing registers.  What a wavefront waits for in the last step of stage i: its own parts of stage i + 1, with
+// kStages - 2 later stages still travelling, then a barrier; behind it stage i + 1 is complete in LDS, and every wavefront has read the last of stage i,
+// whose place the parts of stage i + kStages take.
+// The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for 512 of the reduction, the same way.
 //
 // LDS holds rows of 64 or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
-// different banks, and so do sixteen.
+// different banks, and so do sixteen (no conflicts are counted).
 template <int CHUNKS>
 __device__ __forceinline__ int swizzle(int row) {
     const int b0 = row & 1, b1 = (row >> 1) & 1, b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
@@ -187,25 +188,35 @@ __device__ __forceinline__ void arrived() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int FA, int FB, int MI, int NI>
+template <int FA, int FB, int MI, int NI, int WAVES>
 struct TileShape {
-    static constexpr int TM = 64 * MI, TN = 64 * NI;
-    static constexpr int SUB = FA == DQ_MXFP8 && FB == DQ_MXFP8 ? 1 : 2;              // steps of 64 in a stage
-    static constexpr int RA = kStepBytes<FA> / 2 * SUB, RB = kStepBytes<FB> / 2 * SUB;   // bytes of a row in a stage
-    static constexpr int CA = RA / 16, CB = RB / 16;                     // chunks
-    static constexpr int PA = TM * RA / 4096, PB = TN * RB / 4096;       // transfers of 16 bytes a thread and stage
-    static constexpr int kStageBytes = TM * RA + TN * RB;
-    static constexpr int kScaleBytes = (TM + TN) * 16;
-    static constexpr int kStages = 4 * kStageBytes + kScaleBytes <= 160 * 1024 ? 4 : 3;
-    static constexpr int kLds = kStages * kStageBytes + kScaleBytes;
-    static_assert(kLds <= 160 * 1024, "stages have to fit LDS");
+    static constexpr int kThreads = 64 * WAVES, kPiece = 16 * kThreads;
+    static constexpr int TM = 64 * MI, TN = 16 * WAVES * NI;
+    static constexpr int SUBS = FA == DQ_MXFP4 && FB == DQ_MXFP4 ? 4 : 2;                    // steps of 64 in a stage
+    static constexpr int RA = kStepBytes<FA> / 2 * SUBS, RB = kStepBytes<FB> / 2 * SUBS;        // bytes of a row in a stage
+    static constexpr int CA = RA / 16, CB = RB / 16;                                         // chunks
+    static constexpr int PA = TM * RA / kPiece, kPieces = PA + TN * RB / kPiece;
+    static constexpr int kStageBytes = kPieces * kPiece;
+    // one workgroup a compute unit for the largest tiles, two or three of the smaller ones
+    static constexpr int kScaleSets = MI == 4 ? 1 : 2, kScaleBytes = (TM + TN) * 16;
+    static constexpr int kRoom = (MI == 4 ? 160 : MI == 2 ? 80 : 53) * 1024;
+    static constexpr int kStages = (kRoom - kScaleSets * kScaleBytes) / kStageBytes;
+    static constexpr int kLds = kStages * kStageBytes + kScaleSets * kScaleBytes;
+    static_assert(kStages >= 2, "two stages have to fit");
+    // pieces sent for up to the j-th step behind the barrier: in the first of two steps, in the first two of four
+    static constexpr int sent(int j) { return j < 0 ? 0 : SUBS == 4 && j == 0 ? kPieces / 2 : kPieces; }
+    // transfers that a wavefront may have under way behind stage i + 1; in front of the first read of new scales, no more than were sent for since
+    // those scales, (kScaleSets - 1) * 512 / (64 SUBS) stages and the steps behind a barrier ago
+    static constexpr int kBehind = (kStages - 2) * kPieces;
+    static constexpr int kSinceScales = ((kScaleSets - 1) * 8 / SUBS + 8 / SUBS - 1) * kPieces - sent(0);
+    static constexpr int kBehindScales = kBehind < kSinceScales ? kBehind : kSinceScales;
 };
 
-template <int FA, int FB, class OUT, int MI, int NI>
-__global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
-    using S = TileShape<FA, FB, MI, NI>;
+template <int FA, int FB, class OUT, int MI, int NI, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
+    using S = TileShape<FA, FB, MI, NI, WAVES>;
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
-    constexpr int P = S::PA + S::PB, NST = S::kStages, SUB = S::SUB, BLOCKS = 2 * SUB;      // blocks of a row in a stage
+    constexpr int NP = S::kPieces, NST = S::kStages, SUBS = S::SUBS, BLOCKS = 2 * SUBS;      // blocks of a row in a stage
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, q = lane >> 5;
@@ -228,10 +239,10 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     // this thread's transfers: row and chunk in a tile, as an offset from the tile's first row
     const unsigned char* const baseA = g.A + (long)m0 * g.lda;
     const unsigned char* const baseB = g.B + (long)n0 * g.ldb;
-    unsigned offA[S::PA], offB[S::PB];
+    unsigned offA[S::PA], offB[NP - S::PA];
     int chunkA, chunkB;          // the same for all of a thread's rows, which are 16 or a multiple of it apart
     {
-        constexpr int rows = 256 / S::CA;
+        constexpr int rows = S::kThreads / S::CA;
         const int at = tid / S::CA;
         chunkA = (tid % S::CA) ^ swizzle<S::CA>(at);
 #pragma unroll
@@ -241,20 +252,20 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
         }
     }
     {
-        constexpr int rows = 256 / S::CB;
+        constexpr int rows = S::kThreads / S::CB;
         const int at = tid / S::CB;
         chunkB = (tid % S::CB) ^ swizzle<S::CB>(at);
 #pragma unroll
-        for (int p = 0; p < S::PB; ++p) {
+        for (int p = 0; p < NP - S::PA; ++p) {
             const int row = n0 + p * rows + at < g.N ? p * rows + at : g.N - 1 - n0;
             offB[p] = (unsigned)((long)row * g.ldb) + 16u * chunkB;
         }
     }
-    constexpr int SP = (S::TM + S::TN + 255) / 256;
+    constexpr int SP = (S::TM + S::TN + S::kThreads - 1) / S::kThreads;
     const unsigned char* scale_row[SP];
 #pragma unroll
     for (int p = 0; p < SP; ++p) {
-        const int i = p * 256 + tid;
+        const int i = p * S::kThreads + tid;
         if (i < S::TM) {
             const int row = m0 + i < g.M ? m0 + i : g.M - 1;
             scale_row[p] = g.As + (long)row * g.ldas;
@@ -263,51 +274,60 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
             scale_row[p] = g.Bs + (long)row * g.ldbs;
         }
     }
-    // Piece p of a stage into `place` (a place holds A's rows, then B's).  In the last stage, which stands in for all behind it too, a chunk of a
+    // Piece p of a stage (A's rows, then B's) into the stage's place at `place` in LDS.  In the last stage, which stands in for all behind it too, a chunk of a
     // block that the row does not have is replaced by the row's first one of the stage: its scale counts as 2^-127 in both operands, which makes nothing
     // of any number, and a NaN in it has made the row NaN before.
     const unsigned backA = BLOCKS * (stages - 1) + chunkA / (S::CA / BLOCKS) < nb ? 0u : 16u * chunkA;
     const unsigned backB = BLOCKS * (stages - 1) + chunkB / (S::CB / BLOCKS) < nb ? 0u : 16u * chunkB;
     struct Source { const unsigned char *a, *b; unsigned back_a, back_b; };
     auto source = [&](int t) {
-        const bool last = t >= stages - 1;
-        t = last ? stages - 1 : t;
-        return Source{baseA + (long)t * S::RA, baseB + (long)t * S::RB, last ? backA : 0u, last ? backB : 0u};
+        const bool end = t >= stages - 1;
+        t = end ? stages - 1 : t;
+        return Source{baseA + (long)t * S::RA, baseB + (long)t * S::RB, end ? backA : 0u, end ? backB : 0u};
     };
     auto fetch = [&](const Source& f, int p, int place) {
         const bool a = p < S::PA;
-        const int pp = a ? p : p - S::PA;
-        const unsigned to = smem_at + place * S::kStageBytes + (a ? 0 : S::TM * S::RA) + pp * 4096 + wave * 1024;
-        to_lds(a ? f.a : f.b, a ? offA[a ? pp : 0] - f.back_a : offB[a ? 0 : pp] - f.back_b, to);
+        to_lds(a ? f.a : f.b, a ? offA[a ? p : 0] - f.back_a : offB[a ? 0 : p - S::PA] - f.back_b, smem_at + place + p * S::kPiece + wave * 1024);
     };
     auto fetch_scales = [&](int chunk) {
+        const unsigned to = smem_at + kScalesAt + (S::kScaleSets == 1 ? 0 : (chunk & 1) * S::kScaleBytes) + wave * 1024;
         chunk = 16 * chunk < nb ? chunk : (nb - 1) / 16;
 #pragma unroll
         for (int p = 0; p < SP; ++p)
-            if (S::TM + S::TN >= 256 || wave * 64 < S::TM + S::TN)
-                to_lds(scale_row[p] + 16L * chunk, smem_at + kScalesAt + p * 4096 + wave * 1024);
+            if (S::TM + S::TN >= S::kThreads || wave * 64 < S::TM + S::TN) to_lds(scale_row[p] + 16L * chunk, to + p * S::kPiece);
     };
 
-    const int wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NI;
-    const int rowA = (wm + r) * S::RA, rowB = S::TM * S::RA + (wn + r) * S::RB;
-    const int swA = swizzle<S::CA>(r), swB = swizzle<S::CB>(r);
-
-    Codes<FA> fa[2][MI];
+    const int wm = wave / (WAVES / 2) * 32 * MI, wn = wave % (WAVES / 2) * 32 * NI;
+    // where this lane's 16 bytes of a fragment are, from the start of the fragment's rows: chunks by step, in its two halves for 8 bits
+    auto lane_at = [&](auto fc, auto cc, int row_bytes, int u, int half) {
+        constexpr int F = decltype(fc)::value, C = decltype(cc)::value;
+        const int c = F == DQ_MXFP4 ? 2 * u + q : EXACT ? 4 * u + 2 * q + half : 4 * u + 2 * half + q;
+        return r * row_bytes + 16 * (c ^ swizzle<C>(r));
+    };
+    // a step's multiplications go row by row of A's fragments, so that the next step's can be read over each as soon as its row is done
+    Codes<FA> fa[MI];
     Codes<FB> fb[2][NI];
-    // fragment k (A's, then B's) of step u of the stage at `place`
-    auto read = [&](auto& c, int at, int sw, auto fc, int u) {
-        constexpr int F = decltype(fc)::value;
-        const unsigned char* row = smem + at;
-        if constexpr (F == DQ_MXFP4) {
-            c.a = *reinterpret_cast<const i32x4*>(row + 16 * ((2 * u + q) ^ sw));
-        } else {
-            c.a = *reinterpret_cast<const i32x4*>(row + 16 * ((EXACT ? 4 * u + 2 * q : 4 * u + q) ^ sw));
-            c.b = *reinterpret_cast<const i32x4*>(row + 16 * ((EXACT ? 4 * u + 2 * q + 1 : 4 * u + 2 + q) ^ sw));
+    int lanesA[SUBS][2], lanesB[SUBS][2];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            lanesA[u][half] = wm * S::RA + lane_at(std::integral_constant<int, FA>{}, std::integral_constant<int, S::CA>{}, S::RA, u, half);
+            lanesB[u][half] = S::TM * S::RA + wn * S::RB + lane_at(std::integral_constant<int, FB>{}, std::integral_constant<int, S::CB>{}, S::RB, u, half);
         }
-    };
+    // fragment k (A's, then B's) of step u of the stage at `place`
     auto read_fragment = [&](int k, int set, int u, int place) {
-        if (k < MI) read(fa[set][k], place * S::kStageBytes + rowA + 32 * k * S::RA, swA, std::integral_constant<int, FA>{}, u);
-        else read(fb[set][k - MI], place * S::kStageBytes + rowB + 32 * (k - MI) * S::RB, swB, std::integral_constant<int, FB>{}, u);
+        const unsigned char* at = smem + place;
+        if (k < MI) {
+            Codes<FA>& c = fa[k < MI ? k : 0];
+            c.a = *reinterpret_cast<const i32x4*>(at + lanesA[u][0] + 32 * k * S::RA);
+            if constexpr (FA == DQ_MXFP8) c.b = *reinterpret_cast<const i32x4*>(at + lanesA[u][1] + 32 * k * S::RA);
+        } else {
+            const int j = k < MI ? 0 : k - MI;
+            Codes<FB>& c = fb[set][j];
+            c.a = *reinterpret_cast<const i32x4*>(at + lanesB[u][0] + 32 * j * S::RB);
+            if constexpr (FB == DQ_MXFP8) c.b = *reinterpret_cast<const i32x4*>(at + lanesB[u][1] + 32 * j * S::RB);
+        }
     };
 
     // Scales of 512 of the reduction.  Rows i and i + 1 of fragments: the lanes of the lower half read 16 bytes of a row of fragment i, those of
@@ -317,11 +337,12 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     i32x4 raw[(FR + 1) / 2];
     int sc[FR][2];
     auto frag_row = [&](int k) { return k < MI ? wm + 32 * k : S::TM + wn + 32 * (k - MI); };
-    auto read_scales = [&]() {
+    auto read_scales = [&](int chunk) {
+        const unsigned char* at = smem + kScalesAt + (S::kScaleSets == 1 ? 0 : (chunk & 1) * S::kScaleBytes);
 #pragma unroll
         for (int k = 0; k < FR; k += 2) {
             const int row = q == 0 ? frag_row(k) : frag_row(k + 1 < FR ? k + 1 : k);
-            raw[k / 2] = *reinterpret_cast<const i32x4*>(smem + kScalesAt + 16 * (row + r));
+            raw[k / 2] = *reinterpret_cast<const i32x4*>(at + 16 * (row + r));
         }
     };
     auto place_scales = [&](int chunk) {
@@ -352,71 +373,67 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-    // Step T of the eight of a piece of 512.  From the last step of a stage on its place is filled again (of two steps a stage: half of it there,
-    // half in the first step of the next); that step also reads the next stage's first fragments.  No branches: the instructions stay where they are written, each transfer and read behind a multiplication of its own.
-    constexpr int H = SUB == 1 ? P : P / 2;
-    auto before = [](int x) { return x == 0 ? NST - 1 : x - 1; };
-    int place = 0;
+    // Step T of the eight of a piece of 512.  Behind the barrier in the last step of a stage its place is filled again (and in the next step, if a stage has
+    // four); that step also reads the next stage's first fragments.  No branches: the instructions stay where they are written, each
+    // transfer and read behind a multiplication of its own.
+    int place = 0, freed = (NST - 1) * S::kStageBytes;
     Source from = source(NST - 1);
     auto step = [&](auto tc, int stage) {
-        constexpr int T = decltype(tc)::value, u = T & 1;
-        constexpr bool last = T % SUB == SUB - 1;
-        int next_place = place;
+        constexpr int T = decltype(tc)::value, u = T & 1, sub = T % SUBS;
+        constexpr bool last = sub == SUBS - 1;
         if constexpr (last) {
-            arrived<(NST - 2) * P>();
-            next_place = place + 1 == NST ? 0 : place + 1;
+            arrived<T == 7 ? S::kBehindScales : S::kBehind>();
+            freed = place;
+            place = place == (NST - 1) * S::kStageBytes ? 0 : place + S::kStageBytes;
             from = source(stage + NST);
-            if constexpr (T == 7) read_scales();
+            if constexpr (T == 7) read_scales(stage * SUBS / 8 + 1);
         }
-        constexpr int SLOTS = MI * NI, READS = (FR + SLOTS - 1) / SLOTS;
-        constexpr int first = last ? 0 : H, count = last ? H : P - H;            // transfers of this step
+        constexpr int j = last ? 0 : sub + 1, first = S::sent(j - 1), count = S::sent(j) - first;        // transfers of this step
+        constexpr int SLOTS = MI * NI;
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
             const int i = s / NI, j = (i & 1) ? NI - 1 - s % NI : s % NI;
             if constexpr (EXACT) {
                 const unsigned ea = ((unsigned)sc[i][T / 4] >> (8 * (T & 3))) & 255u, eb = ((unsigned)sc[MI + j][T / 4] >> (8 * (T & 3))) & 255u;
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 0>(fb[u][j], eb), values8<FA, 0>(fa[u][i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 1>(fb[u][j], eb), values8<FA, 1>(fa[u][i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 2>(fb[u][j], eb), values8<FA, 2>(fa[u][i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 3>(fb[u][j], eb), values8<FA, 3>(fa[u][i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 0>(fb[u][j], eb), values8<FA, 0>(fa[i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 1>(fb[u][j], eb), values8<FA, 1>(fa[i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 2>(fb[u][j], eb), values8<FA, 2>(fa[i], ea), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 3>(fb[u][j], eb), values8<FA, 3>(fa[i], ea), acc[i][j], 0, 0, 0);
             } else {
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(fb[u][j]), operand<FA>(fa[u][i]), acc[i][j], kMfmaFormat<FB>,
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(fb[u][j]), operand<FA>(fa[i]), acc[i][j], kMfmaFormat<FB>,
                                                                             kMfmaFormat<FA>, T & 3, sc[MI + j][T / 4], T & 3, sc[i][T / 4]);
             }
+            if (s < NI) read_fragment(MI + s, 1 - u, last ? 0 : sub + 1, place);
+            if (s % NI == NI - 1) read_fragment(i, 0, last ? 0 : sub + 1, place);
 #pragma unroll
-            for (int k = s * READS; k < (s + 1) * READS; ++k)
-                if (k < FR) read_fragment(k, 1 - u, last ? 0 : 1, next_place);
-            // evenly over the step: a wavefront waits where the four send more than the memory path takes in
-#pragma unroll
-            for (int k = count * s / SLOTS; k < count * (s + 1) / SLOTS; ++k) fetch(from, first + k, last ? place : before(place));
+            for (int k = first + count * s / SLOTS; k < first + count * (s + 1) / SLOTS; ++k)
+                fetch(from, k, freed);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (T == 1) fetch_scales(stage * SUB / 8 + 1);
-        if constexpr (last) place = next_place;
-        if constexpr (T == 7) place_scales(stage * SUB / 8 + 1);
+        if constexpr (T == SUBS - 1) fetch_scales(stage * SUBS / 8 + S::kScaleSets);
+        if constexpr (T == 7) place_scales(stage * SUBS / 8 + 1);
     };
 
-    fetch_scales(0);
 #pragma unroll
-    for (int t = 0; t < NST; ++t) {
-        const Source first = source(t);
+    for (int c = 0; c < S::kScaleSets; ++c) fetch_scales(c);
 #pragma unroll
-        for (int p = 0; p < (t + 1 < NST ? P : H); ++p) fetch(first, p, t);
-    }
-    arrived<(NST - 2) * P + H>();
-    read_scales();
+    for (int t = 0; t < NST; ++t)
+#pragma unroll
+        for (int p = 0; p < (t + 1 < NST ? NP : S::sent(0)); ++p) fetch(source(t), p, t * S::kStageBytes);
+    arrived<(NST - 2) * NP + S::sent(0)>();
+    read_scales(0);
 #pragma unroll
     for (int k = 0; k < FR; ++k) read_fragment(k, 0, 0, 0);
     place_scales(0);
-    for (int stage = 0; stage < stages; stage += 8 / SUB) {
+    for (int stage = 0; stage < stages; stage += 8 / SUBS) {
         step(std::integral_constant<int, 0>{}, stage);
-        step(std::integral_constant<int, 1>{}, stage + 1 / SUB);
-        step(std::integral_constant<int, 2>{}, stage + 2 / SUB);
-        step(std::integral_constant<int, 3>{}, stage + 3 / SUB);
-        step(std::integral_constant<int, 4>{}, stage + 4 / SUB);
-        step(std::integral_constant<int, 5>{}, stage + 5 / SUB);
-        step(std::integral_constant<int, 6>{}, stage + 6 / SUB);
-        step(std::integral_constant<int, 7>{}, stage + 7 / SUB);
+        step(std::integral_constant<int, 1>{}, stage + 1 / SUBS);
+        step(std::integral_constant<int, 2>{}, stage + 2 / SUBS);
+        step(std::integral_constant<int, 3>{}, stage + 3 / SUBS);
+        step(std::integral_constant<int, 4>{}, stage + 4 / SUBS);
+        step(std::integral_constant<int, 5>{}, stage + 5 / SUBS);
+        step(std::integral_constant<int, 6>{}, stage + 6 / SUBS);
+        step(std::integral_constant<int, 7>{}, stage + 7 / SUBS);
     }
     arrived<0>();        // nothing may still be on its way into LDS when the workgroup ends
 
@@ -467,12 +484,12 @@ __global__ __launch_bounds__(256) void gemm_mx_tile_kernel(GemmMx g, int tiles_m
     }
 }
 
-template <int FA, int FB, class OUT, int MI, int NI>
+template <int FA, int FB, class OUT, int MI, int NI, int WAVES>
 hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
-    using S = TileShape<FA, FB, MI, NI>;
+    using S = TileShape<FA, FB, MI, NI, WAVES>;
     const long tm = (g.M + (long)S::TM - 1) / S::TM, tn = (g.N + (long)S::TN - 1) / S::TN;
     if (tm * tn > 0x7fffffffL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gemm_mx_tile_kernel<FA, FB, OUT, MI, NI>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, g, (int)tm, (int)tn);
+    hipLaunchKernelGGL((gemm_mx_tile_kernel<FA, FB, OUT, MI, NI, WAVES>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, g, (int)tm, (int)tn);
     return hipGetLastError();
 }
 
@@ -485,9 +502,9 @@ hipError_t launch_types(const GemmMx& g, hipStream_t s) {
         const long t256 = ((g.M + 255L) / 256) * ((g.N + 255L) / 256), t128 = ((g.M + 127L) / 128) * ((g.N + 127L) / 128);
         constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
         if constexpr (!exact)
-            if (t256 >= 192) return launch_tile<FA, FB, OUT, 4, 4>(g, s);
-        if (t128 >= 192) return launch_tile<FA, FB, OUT, 2, 2>(g, s);
-        return launch_tile<FA, FB, OUT, 1, 1>(g, s);
+            if (t256 >= 192) { if (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8>(g, s); return launch_tile<FA, FB, OUT, 4, 4, 4>(g, s); }
+        if (t128 >= 192) return launch_tile<FA, FB, OUT, 2, 2, 4>(g, s);
+        return launch_tile<FA, FB, OUT, 1, 1, 4>(g, s);
     }
     if (g.M <= 16) hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 1>), dim3(gx, 1), dim3(512), 0, s, g);
     else hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 4>), dim3(gx, (unsigned)((g.M + 63L) / 64)), dim3(512), 0, s, g);
