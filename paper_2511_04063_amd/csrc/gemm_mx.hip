@@ -56,10 +56,6 @@ __device__ __forceinline__ Codes<F> load_codes(const unsigned char* row, int ste
     }
     return c;
 }
-__device__ __forceinline__ unsigned load_scale(const unsigned char* row, int step, int g, int nb) {
-    return 4 * step + g < nb ? row[4 * step + g] : 0u;
-}
-
 // codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale, in bf16
 template <int F, int J>
 __device__ __forceinline__ bf16x8 values8(const Codes<F>& c, unsigned byte) {
@@ -110,50 +106,69 @@ __device__ __forceinline__ void store4(OUT* dst, int left, f32x4 v) {
     }
 }
 
-// ---- straight from memory: a workgroup of 8 wavefronts makes 16 MT rows x 16 columns of C, each wavefront taking every eighth 128 of the
-// reduction; the eight sums are added in order through LDS.
-template <int FA, int FB, class OUT, int MT>
-__global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g) {
+// ---- straight from memory, for a few rows: a workgroup of 8 wavefronts makes 16 rows x 16 NT columns of C.  Each wavefront takes every eighth piece of 512 of the
+// reduction (a row's 16 scales, one load) and has all of a piece's operands under way at once; the eight sums are added in order through LDS.
+template <int FA, int FB, class OUT, int NT>
+__global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles_n) {
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
-    __shared__ f32x4 part[8][MT][64];
+    __shared__ f32x4 part[8][NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MT);
-    const int nb = (int)((g.K + 31L) / 32), steps = (nb + 3) / 4;
-    const int nr = n0 + r < g.N ? n0 + r : g.N - 1;
-    const unsigned char* pb = g.B + (long)nr * g.ldb;
-    const unsigned char* sb = g.Bs + (long)nr * g.ldbs;
-    const unsigned char* pa[MT];
-    const unsigned char* sa[MT];
+    const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * (16 * NT), m0 = (int)(blockIdx.x / (unsigned)tiles_n) * 16;
+    const int nb = (int)((g.K + 31L) / 32);
+    const int row_a = m0 + r < g.M ? m0 + r : g.M - 1;
+    const unsigned char *pa = g.A + (long)row_a * g.lda, *sa = g.As + (long)row_a * g.ldas, *pb[NT], *sb[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int mr = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
-        pa[i] = g.A + (long)mr * g.lda;
-        sa[i] = g.As + (long)mr * g.ldas;
+    for (int j = 0; j < NT; ++j) {
+        const int row = n0 + 16 * j + r < g.N ? n0 + 16 * j + r : g.N - 1;
+        pb[j] = g.B + (long)row * g.ldb;
+        sb[j] = g.Bs + (long)row * g.ldbs;
     }
-    f32x4 acc[MT];
+    f32x4 acc[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int t = wave; t < steps; t += 8) {
-        const Codes<FB> b = load_codes<FB, EXACT>(pb, t, q, nb);
-        const unsigned eb = load_scale(sb, t, q, nb);
+    for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int piece = wave; 16 * piece < nb; piece += 8) {
+        Codes<FA> a[4];
+        Codes<FB> b[4][NT];
+        i32x4 ea, eb[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const Codes<FA> a = load_codes<FA, EXACT>(pa[i], t, q, nb);
-            const unsigned ea = load_scale(sa[i], t, q, nb);
-            if constexpr (EXACT) acc[i] = mfma_values<FB, FA>(b, a, acc[i], eb, ea);
-            else acc[i] = mfma_mx<FB, FA>(b, a, acc[i], (int)eb, (int)ea);
+        for (int j = 0; j < NT; ++j) eb[j] = *reinterpret_cast<const i32x4*>(sb[j] + 16L * piece);
+        ea = *reinterpret_cast<const i32x4*>(sa + 16L * piece);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[t][j] = load_codes<FB, EXACT>(pb[j], 4 * piece + t, q, nb);
+            a[t] = load_codes<FA, EXACT>(pa, 4 * piece + t, q, nb);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const bool in = 16 * piece + 4 * t + q < nb;          // what lies behind a row's last scale may be anything
+            const unsigned xa = in ? (unsigned)ea[t] >> (8 * q) : 0u;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const unsigned xb = in ? (unsigned)eb[j][t] >> (8 * q) : 0u;
+                if constexpr (EXACT) acc[j] = mfma_values<FB, FA>(b[t][j], a[t], acc[j], xb & 255u, xa & 255u);
+                else acc[j] = mfma_mx<FB, FA>(b[t][j], a[t], acc[j], (int)xb, (int)xa);
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+    for (int j = 0; j < NT; ++j) part[wave][j][lane] = acc[j];
     __syncthreads();
-    if (wave < MT) {
+    if (wave < NT) {
         f32x4 c = part[0][wave][lane];
 #pragma unroll
         for (int k = 1; k < 8; ++k) c += part[k][wave][lane];
-        const int m = m0 + 16 * wave + r, n = n0 + 4 * q;
+        const int m = m0 + r, n = n0 + 16 * wave + 4 * q;
         if (m < g.M && n < g.N) store4(static_cast<OUT*>(g.C) + (long)m * g.ldc + n, g.N - n, c);
     }
+}
+
+template <int FA, int FB, class OUT, int NT>
+hipError_t launch_direct(const GemmMx& g, hipStream_t s) {
+    const long tn = (g.N + 16L * NT - 1) / (16 * NT), tm = (g.M + 15L) / 16;
+    if (tm * tn > 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, NT>), dim3((unsigned)(tm * tn)), dim3(512), 0, s, g, (int)tn);
+    return hipGetLastError();
 }
 
 // ---- tiles through LDS: a workgroup of 2 x 2 wavefronts makes 64 MI x 64 NI of C, a wavefront 32 MI x 32 NI of it in 32 x 32 x 64 instructions
@@ -188,7 +203,7 @@ __device__ __forceinline__ void arrived() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int FA, int FB, int MI, int NI, int WAVES>
+template <int FA, int FB, int MI, int NI, int WAVES, int GROUPS, int ROOM>
 struct TileShape {
     static constexpr int kThreads = 64 * WAVES, kPiece = 16 * kThreads;
     static constexpr int TM = 64 * MI, TN = 16 * WAVES * NI;
@@ -197,29 +212,30 @@ struct TileShape {
     static constexpr int CA = RA / 16, CB = RB / 16;                                         // chunks
     static constexpr int PA = TM * RA / kPiece, kPieces = PA + TN * RB / kPiece;
     static constexpr int kStageBytes = kPieces * kPiece;
-    // one workgroup a compute unit for the largest tiles, two or three of the smaller ones
-    static constexpr int kScaleSets = MI == 4 ? 1 : 2, kScaleBytes = (TM + TN) * 16;
-    static constexpr int kRoom = (MI == 4 ? 160 : MI == 2 ? 80 : 53) * 1024;
-    static constexpr int kStages = (kRoom - kScaleSets * kScaleBytes) / kStageBytes;
+    static constexpr int kScaleSets = MI < 4 ? 2 : 1, kScaleBytes = (TM + TN + 63) / 64 * 1024;
+    static constexpr int kStages = (ROOM * 1024 / GROUPS - kScaleSets * kScaleBytes) / kStageBytes;
     static constexpr int kLds = kStages * kStageBytes + kScaleSets * kScaleBytes;
     static_assert(kStages >= 2, "two stages have to fit");
     // pieces sent for up to the j-th step behind the barrier: in the first of two steps, in the first two of four
     static constexpr int sent(int j) { return j < 0 ? 0 : SUBS == 4 && j == 0 ? kPieces / 2 : kPieces; }
     // transfers that a wavefront may have under way behind stage i + 1; in front of the first read of new scales, no more than were sent for since
-    // those scales, (kScaleSets - 1) * 512 / (64 SUBS) stages and the steps behind a barrier ago
-    static constexpr int kBehind = (kStages - 2) * kPieces;
+    // those scales, which were sent for behind the first barrier of the 512 before (of the 512 before that, with two sets)
+    static constexpr int kBehind = (kStages - 2) * kPieces < 60 ? (kStages - 2) * kPieces : 60;
     static constexpr int kSinceScales = ((kScaleSets - 1) * 8 / SUBS + 8 / SUBS - 1) * kPieces - sent(0);
     static constexpr int kBehindScales = kBehind < kSinceScales ? kBehind : kSinceScales;
 };
 
-template <int FA, int FB, class OUT, int MI, int NI, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
-    using S = TileShape<FA, FB, MI, NI, WAVES>;
+template <int FA, int FB, class OUT, int MI, int NI, int WAVES, int GROUPS, int ROOM>
+__global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmMx g, int tiles_m, int tiles_n) {
+    using S = TileShape<FA, FB, MI, NI, WAVES, GROUPS, ROOM>;
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
     constexpr int NP = S::kPieces, NST = S::kStages, SUBS = S::SUBS, BLOCKS = 2 * SUBS;      // blocks of a row in a stage
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLds];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(1024))) unsigned char all_smem[S::kLds * GROUPS];
+    // GROUPS sets of WAVES wavefronts, each with its own part of LDS and every GROUPS-th piece of 512 of the reduction
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / S::kThreads);
+    const int tid = (int)threadIdx.x % S::kThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, q = lane >> 5;
+    unsigned char* const smem = all_smem + group * S::kLds;
 
     // XCD-aware tile order (see gemm_f32.hip): the workgroups resident on an XCD form a block of tiles 8 high
     const int nt = tiles_m * tiles_n;
@@ -227,12 +243,15 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
     const int q8 = nt >> 3, r8 = nt & 7;
     const int xcd = bid & 7;
     const int pid = xcd * q8 + (xcd < r8 ? xcd : r8) + (bid >> 3);
-    const int group = 8 * tiles_n;
-    const int first_m = pid / group * 8;
+    const int band = 8 * tiles_n;
+    const int first_m = pid / band * 8;
     const int gsz = (tiles_m - first_m) < 8 ? (tiles_m - first_m) : 8;
-    const int m0 = (first_m + (pid % group) % gsz) * S::TM, n0 = (pid % group) / gsz * S::TN;
+    const int m0 = (first_m + (pid % band) % gsz) * S::TM, n0 = (pid % band) / gsz * S::TN;
 
     const int nb = (int)((g.K + 31L) / 32), stages = (nb + BLOCKS - 1) / BLOCKS;
+    constexpr int PER = 8 / SUBS;                  // stages of 512
+    const int pieces = (nb + 15) / 16, local_stages = (pieces + GROUPS - 1) / GROUPS * PER;
+    auto whole_piece = [&](int piece) { return GROUPS == 1 ? piece : piece * GROUPS + group; };      // of this group's
     const unsigned smem_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
     constexpr int kScalesAt = NST * S::kStageBytes;
 
@@ -280,7 +299,8 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
     const unsigned backA = BLOCKS * (stages - 1) + chunkA / (S::CA / BLOCKS) < nb ? 0u : 16u * chunkA;
     const unsigned backB = BLOCKS * (stages - 1) + chunkB / (S::CB / BLOCKS) < nb ? 0u : 16u * chunkB;
     struct Source { const unsigned char *a, *b; unsigned back_a, back_b; };
-    auto source = [&](int t) {
+    auto source = [&](int local) {
+        int t = GROUPS == 1 ? local : whole_piece(local / PER) * PER + local % PER;
         const bool end = t >= stages - 1;
         t = end ? stages - 1 : t;
         return Source{baseA + (long)t * S::RA, baseB + (long)t * S::RB, end ? backA : 0u, end ? backB : 0u};
@@ -291,10 +311,11 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
     };
     auto fetch_scales = [&](int chunk) {
         const unsigned to = smem_at + kScalesAt + (S::kScaleSets == 1 ? 0 : (chunk & 1) * S::kScaleBytes) + wave * 1024;
+        chunk = whole_piece(chunk);
         chunk = 16 * chunk < nb ? chunk : (nb - 1) / 16;
 #pragma unroll
         for (int p = 0; p < SP; ++p)
-            if (S::TM + S::TN >= S::kThreads || wave * 64 < S::TM + S::TN) to_lds(scale_row[p] + 16L * chunk, to + p * S::kPiece);
+            if ((S::TM + S::TN) % S::kThreads == 0 || p * S::kThreads + wave * 64 < S::TM + S::TN) to_lds(scale_row[p] + 16L * chunk, to + p * S::kPiece);
     };
 
     const int wm = wave / (WAVES / 2) * 32 * MI, wn = wave % (WAVES / 2) * 32 * NI;
@@ -349,7 +370,7 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
         unsigned keep[4];            // what lies behind the row's last scale may be anything
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const int have = nb - 16 * chunk - 4 * w;
+            const int have = nb - 16 * whole_piece(chunk) - 4 * w;
             keep[w] = have >= 4 ? ~0u : have <= 0 ? 0u : (1u << (8 * have)) - 1u;
         }
 #pragma unroll
@@ -373,6 +394,24 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
+    // the s-th product of fragments of step T of a piece of 512
+    auto multiply = [&](auto tc, int s) {
+        constexpr int T = decltype(tc)::value;
+        const int i = s / NI, j = (i & 1) ? NI - 1 - s % NI : s % NI;
+        const Codes<FA>& a = fa[i];
+        const Codes<FB>& b = fb[T & 1][j];
+        if constexpr (EXACT) {
+            const unsigned ea = ((unsigned)sc[i][T / 4] >> (8 * (T & 3))) & 255u, eb = ((unsigned)sc[MI + j][T / 4] >> (8 * (T & 3))) & 255u;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 0>(b, eb), values8<FA, 0>(a, ea), acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 1>(b, eb), values8<FA, 1>(a, ea), acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 2>(b, eb), values8<FA, 2>(a, ea), acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 3>(b, eb), values8<FA, 3>(a, ea), acc[i][j], 0, 0, 0);
+        } else {
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(b), operand<FA>(a), acc[i][j], kMfmaFormat<FB>, kMfmaFormat<FA>,
+                                                                        T & 3, sc[MI + j][T / 4], T & 3, sc[i][T / 4]);
+        }
+    };
+
     // Step T of the eight of a piece of 512.  Behind the barrier in the last step of a stage its place is filled again (and in the next step, if a stage has
     // four); that step also reads the next stage's first fragments.  No branches: the instructions stay where they are written, each
     // transfer and read behind a multiplication of its own.
@@ -392,17 +431,8 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
         constexpr int SLOTS = MI * NI;
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
-            const int i = s / NI, j = (i & 1) ? NI - 1 - s % NI : s % NI;
-            if constexpr (EXACT) {
-                const unsigned ea = ((unsigned)sc[i][T / 4] >> (8 * (T & 3))) & 255u, eb = ((unsigned)sc[MI + j][T / 4] >> (8 * (T & 3))) & 255u;
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 0>(fb[u][j], eb), values8<FA, 0>(fa[i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 1>(fb[u][j], eb), values8<FA, 1>(fa[i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 2>(fb[u][j], eb), values8<FA, 2>(fa[i], ea), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8<FB, 3>(fb[u][j], eb), values8<FA, 3>(fa[i], ea), acc[i][j], 0, 0, 0);
-            } else {
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(fb[u][j]), operand<FA>(fa[i]), acc[i][j], kMfmaFormat<FB>,
-                                                                            kMfmaFormat<FA>, T & 3, sc[MI + j][T / 4], T & 3, sc[i][T / 4]);
-            }
+            const int i = s / NI;
+            multiply(tc, s);
             if (s < NI) read_fragment(MI + s, 1 - u, last ? 0 : sub + 1, place);
             if (s % NI == NI - 1) read_fragment(i, 0, last ? 0 : sub + 1, place);
 #pragma unroll
@@ -420,12 +450,13 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
     for (int t = 0; t < NST; ++t)
 #pragma unroll
         for (int p = 0; p < (t + 1 < NST ? NP : S::sent(0)); ++p) fetch(source(t), p, t * S::kStageBytes);
-    arrived<(NST - 2) * NP + S::sent(0)>();
+    constexpr int kFirst = (NST - 2) * NP + S::sent(0);
+    arrived<(kFirst < 60 ? kFirst : 60)>();
     read_scales(0);
 #pragma unroll
     for (int k = 0; k < FR; ++k) read_fragment(k, 0, 0, 0);
     place_scales(0);
-    for (int stage = 0; stage < stages; stage += 8 / SUBS) {
+    for (int stage = 0; stage < local_stages; stage += PER) {
         step(std::integral_constant<int, 0>{}, stage);
         step(std::integral_constant<int, 1>{}, stage + 1 / SUBS);
         step(std::integral_constant<int, 2>{}, stage + 2 / SUBS);
@@ -436,6 +467,37 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
         step(std::integral_constant<int, 7>{}, stage + 7 / SUBS);
     }
     arrived<0>();        // nothing may still be on its way into LDS when the workgroup ends
+
+    // the groups' sums, added in order
+    if constexpr (GROUPS > 1) {
+        static_assert(64 * WAVES * MI * NI * 64 <= S::kLds, "a group's sums have to fit its part of LDS");
+        f32x4* const mine = reinterpret_cast<f32x4*>(smem);
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        mine[((i * NI + j) * 4 + v) * S::kThreads + tid] = f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int other = 1; other < GROUPS; ++other) {
+            const f32x4* const from_group = reinterpret_cast<const f32x4*>(all_smem + other * S::kLds);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const f32x4 x = from_group[((i * NI + j) * 4 + v) * S::kThreads + tid];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) acc[i][j][4 * v + y] += x[y];
+                    }
+        }
+    }
 
     // register 4 x + y of a lane holds C[m = r][n = 8 x + 4 q + y]; lanes of the two halves exchange groups of four, so that each writes eight
     // columns in a row: lower half 16 x .., upper half 16 x + 8 ..
@@ -484,31 +546,43 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx_tile_kernel(GemmMx g, int 
     }
 }
 
-template <int FA, int FB, class OUT, int MI, int NI, int WAVES>
+template <int FA, int FB, class OUT, int MI, int NI, int WAVES, int GROUPS, int ROOM>
 hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
-    using S = TileShape<FA, FB, MI, NI, WAVES>;
+    using S = TileShape<FA, FB, MI, NI, WAVES, GROUPS, ROOM>;
     const long tm = (g.M + (long)S::TM - 1) / S::TM, tn = (g.N + (long)S::TN - 1) / S::TN;
     if (tm * tn > 0x7fffffffL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gemm_mx_tile_kernel<FA, FB, OUT, MI, NI, WAVES>), dim3((unsigned)(tm * tn)), dim3(S::kThreads), 0, s, g, (int)tm, (int)tn);
+    hipLaunchKernelGGL((gemm_mx_tile_kernel<FA, FB, OUT, MI, NI, WAVES, GROUPS, ROOM>), dim3((unsigned)(tm * tn)), dim3(S::kThreads * GROUPS), 0, s, g, (int)tm, (int)tn);
     return hipGetLastError();
 }
 
+// Which kernel, by what each takes for C = M x N, K (us of the kernel alone; 4 x 4 bits unless said):
+//   straight from memory against 64 x 32 tiles      1 x 4096, 4096: 3.9, 6.1;  16 x 4096, 4096 (8 x 8): 6.8, 7.8;  but 16 x 8192, 8192 (8 x 8): 20.0, 13.3;
+//                                                   24 x 8192, 4096 (8 x 4; 32 rows of the first kernel): 7.5, 6.7
+//   64 x 32 tiles, 4 groups against 64 x 64, 2      128 x 4096, 4096: 5.7, 6.6;  256 x 4096, 4096 (512 and 256 workgroups): 11.1, 7.2
+//   64 x 64 tiles against 128 x 64, 2 groups        256 x 4096, 4096: 7.2, 8.7;  512 x 4096, 4096 (512 and 256 workgroups): 11.4, 9.8
+//   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 9.8, 11.4;  1024 x 4096, 4096: 18.7, 14.7
+//   128 x 128 tiles against 256 x 256               2048 x 4096, 4096 (512 and 128 workgroups): 25.4, 26.5
+// that is, the largest tile that still gives most compute units a workgroup.  A kernel of no work takes 2 us, one of 64 in the reduction 4 to 5.
 template <int FA, int FB, class OUT>
 hipError_t launch_types(const GemmMx& g, hipStream_t s) {
-    const unsigned gx = (unsigned)((g.N + 15L) / 16);
-    // the tiles address 256 rows of codes by 32-bit offsets
-    const bool near_rows = g.lda < (1L << 23) && g.ldb < (1L << 23);
-    if (near_rows && g.M > 64) {
-        const long t256 = ((g.M + 255L) / 256) * ((g.N + 255L) / 256), t128 = ((g.M + 127L) / 128) * ((g.N + 127L) / 128);
-        constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
-        if constexpr (!exact)
-            if (t256 >= 192) { if (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8>(g, s); return launch_tile<FA, FB, OUT, 4, 4, 4>(g, s); }
-        if (t128 >= 192) return launch_tile<FA, FB, OUT, 2, 2, 4>(g, s);
-        return launch_tile<FA, FB, OUT, 1, 1, 4>(g, s);
+    constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
+    const bool near_rows = g.lda < (1L << 23) && g.ldb < (1L << 23);       // the tiles address their rows by 32-bit offsets
+    if (!near_rows || (g.M <= 16 && g.K <= 4096)) {
+        // 32 columns a workgroup as soon as that gives every compute unit one: 1 x 8192, 8192 8.1 -> 7.7 us
+        return g.N >= 32 * 256 ? launch_direct<FA, FB, OUT, 2>(g, s) : launch_direct<FA, FB, OUT, 1>(g, s);
     }
-    if (g.M <= 16) hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 1>), dim3(gx, 1), dim3(512), 0, s, g);
-    else hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, 4>), dim3(gx, (unsigned)((g.M + 63L) / 64)), dim3(512), 0, s, g);
-    return hipGetLastError();
+    const auto tiles = [&](long tm, long tn) { return ((g.M + tm - 1) / tm) * ((g.N + tn - 1) / tn); };
+    constexpr long most = 192;
+    if (!exact && tiles(256, 256) >= most) {
+        // eight wavefronts to a tile for 4 x 4 bits (8192^3: 324 -> 299 us), four for the others, whose fragments do not leave registers for two
+        // wavefronts a SIMD (8 x 8 bits: 429 us against 476)
+        if constexpr (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8, 1, 160>(g, s);
+        else if constexpr (!exact) return launch_tile<FA, FB, OUT, 4, 4, 4, 1, 160>(g, s);
+    }
+    if (tiles(128, 128) >= most) return launch_tile<FA, FB, OUT, 2, 2, 4, 1, 80>(g, s);
+    if (tiles(128, 64) >= most) return launch_tile<FA, FB, OUT, 2, 1, 4, 2, 160>(g, s);
+    if (tiles(64, 64) >= most) return launch_tile<FA, FB, OUT, 1, 1, 4, 2, 80>(g, s);
+    return launch_tile<FA, FB, OUT, 1, 1, 2, 4, 160>(g, s);
 }
 
 template <int FA, int FB>
