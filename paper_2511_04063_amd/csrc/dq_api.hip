@@ -1143,7 +1143,7 @@ dq_status rotate_loss_grad_one(dq_ctx* c, const Layout& L, int T, int n, const v
     // S4: loss and dY in one pass over Y
     if (!fused) {
         const bool whip = c->objective == DQ_OBJ_WHIP;
-        const int grid = whip ? whip_grid(T, n) : objective_grid(T, n);
+        const int grid = whip ? whip_grid(T, n) : objective_grid(c->objective, T, n);
         const double bytes = (double)T * n * (4.0 + (xdt == DQ_BF16 ? 2.0 : 4.0));
         {
             LaunchScope sc(&c->prof, s, DQ_K_WHIP, 5.0 * T * (double)n, bytes);
@@ -1998,7 +1998,7 @@ dq_status dq_objective_loss_grad(dq_ctx* c, dq_objective objective, int quant_bi
     const float scale = (red == DQ_REDUCE_TOKEN_MEAN) ? 1.f / (float)T : 1.f;
     const size_t esz = dY == nullptr ? 0 : ((dydt == DQ_BF16) ? 2 : 4);
     if (b == 0) return DQ_OK;
-    int grid = objective_grid(T, n);
+    int grid = objective_grid(objective, T, n);
     if ((long)grid * b > kLossPartials) grid = kLossPartials / b;
     if (grid < 1) return DQ_ERR_UNSUPPORTED;
     {

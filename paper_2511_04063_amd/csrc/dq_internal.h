@@ -361,7 +361,7 @@ hipError_t launch_loss_finish(const double* partials, int count, float scale, fl
                               hipStream_t s, int batch = 1, unsigned* small = nullptr);
 
 // Row-wise objectives (1 variance, 2 kurtosis, 3 quantisation error): one partial per workgroup like the Whip pass.
-int objective_grid(int T, int n);
+int objective_grid(int objective, int T, int n);
 hipError_t launch_objective(int objective, int bits, const float* Y, long ldy, int T, int n, float scale, void* dY,
                             int dy_is_bf16, long lddy, double* partials, int grid, hipStream_t s, int batch = 1,
                             long stride_y = 0, long stride_dy = 0);
@@ -384,6 +384,7 @@ struct MxNorm {
 };
 hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s);
 // as launch_objective; 16-byte aligned rows of Y and (8-byte in bf16) of dY
+int mx_objective_grid(int T, int n);
 hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy);
 struct GemmMx {

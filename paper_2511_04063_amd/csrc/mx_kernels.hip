@@ -10,35 +10,46 @@ template <class T> struct Piece;                       // what one 16-byte acces
 template <> struct Piece<float> { static constexpr int V = 4; };
 template <> struct Piece<bf16_t> { static constexpr int V = 8; };
 
-__device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
 __device__ __forceinline__ unsigned bf16_pair(float a, float b) {
     const mx_f32x2 v = {a, b};
     return __builtin_bit_cast(unsigned, __builtin_convertvector(v, mx_bf16x2));
 }
 
-// The piece of a row at src with `left` columns to the row's end (possibly none); columns behind it read as zeros.  Nothing behind the
-// row's end is touched.
-__device__ __forceinline__ void load_piece(const float* src, int left, float (&v)[4]) {
-    if (left >= 4) {
-        const float4 q = *reinterpret_cast<const float4*>(src);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-    } else {
+// What a 16-byte access brings: raw until all of a thread's are under way.
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
+    const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < left ? src[i] : 0.f;
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void load_piece(const bf16_t* src, int left, float (&v)[8]) {
-    if (left >= 8) {
-        const uint4 q = *reinterpret_cast<const uint4*>(src);
-        const unsigned w[4] = {q.x, q.y, q.z, q.w};
+// The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  Whole pieces without a
+// branch (a piece that is none reads the row's first one instead, and is cleared); with RAGGED, n no multiple of V, the row's last piece again
+// value by value.
+template <class T>
+__device__ __forceinline__ uint4 load_whole(const T* row, int c, int n) {
+    constexpr int V = Piece<T>::V;
+    return n >= V ? *reinterpret_cast<const uint4*>(row + (c + V <= n ? c : 0)) : make_uint4(0u, 0u, 0u, 0u);
+}
+template <bool RAGGED, class T>
+__device__ __forceinline__ void finish_piece(uint4& q, const T* row, int c, int n) {
+    constexpr int V = Piece<T>::V;
+    if (c + V > n) {
+        q = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (RAGGED) {
+            unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16_value(w[i] & 0xffffu);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            for (int i = 0; i < V - 1; ++i)
+                if (c + i < n) {
+                    if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
+                    else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+                }
+            q = make_uint4(w[0], w[1], w[2], w[3]);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_value(src[i]) : 0.f;
     }
 }
 __device__ __forceinline__ void store_piece(float* dst, int left, const float (&v)[4]) {
@@ -115,17 +126,27 @@ __device__ __forceinline__ bool walk_start(const Walk& w, int& row, int& unit) {
     return unit < w.upr;
 }
 
-template <class IN, int F>
+// U rows of a thread under way at a time
+template <class IN, int F, bool RAGGED>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__ X, long ldx, int T, int n, int nb, unsigned char* __restrict__ codes,
                                                           long ldc, unsigned char* __restrict__ scales, long lds, Walk w, unsigned* flags) {
-    constexpr int V = Piece<IN>::V;
+    constexpr int V = Piece<IN>::V, U = 4;
     int row, unit;
     if (!walk_start(w, row, unit)) return;
-    const int step = w.rg * (int)gridDim.y, left = n - unit * V;
-    for (long r = row; r < T; r += step) {
-        float v[V];
-        load_piece(X + r * ldx + (long)unit * V, left, v);
-        put_blocks<F, V>(v, unit, nb, codes + r * ldc, scales + r * lds, flags);
+    const long step = (long)w.rg * gridDim.y;
+    for (long r = row; r < T; r += U * step) {
+        uint4 q[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) q[k] = load_whole(X + (r + k * step < T ? r + k * step : r) * ldx, unit * V, n);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const long at = r + k * step;
+            if (at >= T) break;
+            finish_piece<RAGGED>(q[k], X + at * ldx, unit * V, n);
+            float v[V];
+            unpack(q[k], v);
+            put_blocks<F, V>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
+        }
     }
 }
 
@@ -159,9 +180,15 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const unsigned char*
     }
 }
 
+template <int OFF>
+__device__ __forceinline__ double lane_xor_double(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = __float_as_uint(lane_xor<OFF>(__uint_as_float((unsigned)u))), hi = __float_as_uint(lane_xor<OFF>(__uint_as_float((unsigned)(u >> 32))));
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    v += lane_xor_double<1>(v); v += lane_xor_double<2>(v); v += lane_xor_double<8>(v);
+    v += lane_xor_double<4>(v); v += lane_xor_double<16>(v); v += lane_xor_double<32>(v);
     return v;
 }
 
@@ -177,38 +204,59 @@ __device__ __forceinline__ double inverse_root(double m) {
 // One token row per TPR threads, P pieces each:  h = x + res (rounded to the stored type: the norm is that of what is stored),
 // y = fp32(h / sqrt(mean h^2 + eps) * gain), then MX blocks of y.  The mean and y are formed in 64 bits and rounded once: a difference in
 // the last bit of y flips codes next to a border, and a row's sum in 32 bits moves every value of the row.  H may be X or res.
-template <class IN, int F, int P, int TPR>
+template <class IN, int F, int P, int TPR, bool RAGGED>
 __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx, const IN* res, long ldr, IN* H, long ldh, const float* __restrict__ gain,
                                                           float eps, int T, int n, int nb, unsigned char* __restrict__ codes, long ldc,
                                                           unsigned char* __restrict__ scales, long lds, unsigned* flags) {
     constexpr int V = Piece<IN>::V, ROWS = 256 / TPR;
     __shared__ double part[4];
     const int t = (int)threadIdx.x % TPR;
-    const long row = (long)blockIdx.x * ROWS + (int)threadIdx.x / TPR;
+    const long row = (long)blockIdx.x * ROWS + (int)threadIdx.x / TPR, at = row < T ? row : T - 1;
     const bool live = row < T;
-    float h[P][V];
+    uint4 q[P], z[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) q[p] = load_whole(X + at * ldx, (p * TPR + t) * V, n);
+    if (res != nullptr) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) z[p] = load_whole(res + at * ldr, (p * TPR + t) * V, n);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (p * TPR + t) * V;
+            finish_piece<RAGGED>(q[p], X + at * ldx, c, n);
+            finish_piece<RAGGED>(z[p], res + at * ldr, c, n);
+            float h[V], r[V];
+            unpack(q[p], h);
+            unpack(z[p], r);
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[i] += r[i];
+            if constexpr (V == 8) q[p] = make_uint4(bf16_pair(h[0], h[1]), bf16_pair(h[2], h[3]), bf16_pair(h[4], h[5]), bf16_pair(h[6], h[7]));
+            else q[p] = make_uint4(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3]));
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) finish_piece<RAGGED>(q[p], X + at * ldx, (p * TPR + t) * V, n);
+    }
     double ss = 0.0;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int c = (p * TPR + t) * V, left = live ? n - c : 0;
-        if (left > 0) {
-            load_piece(X + row * ldx + c, left, h[p]);
-            if (res != nullptr) {
-                float r[V];
-                load_piece(res + row * ldr + c, left, r);
+        const int c = (p * TPR + t) * V;
+        if (H != nullptr && live) {
+            if (c + V <= n) {
+                *reinterpret_cast<uint4*>(H + row * ldh + c) = q[p];
+            } else if (RAGGED && c < n) {
+                const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    h[p][i] += r[i];
-                    if constexpr (V == 8) h[p][i] = (float)(__bf16)h[p][i];
-                }
+                for (int i = 0; i < V - 1; ++i)
+                    if (c + i < n) {
+                        if constexpr (V == 4) H[row * ldh + c + i] = __uint_as_float(w[i]);
+                        else H[row * ldh + c + i] = (bf16_t)(w[i / 2] >> (16 * (i & 1)));
+                    }
             }
-            if (H != nullptr) store_piece(H + row * ldh + c, left, h[p]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) h[p][i] = 0.f;
         }
+        float h[V];
+        unpack(q[p], h);
 #pragma unroll
-        for (int i = 0; i < V; ++i) ss += (double)h[p][i] * (double)h[p][i];
+        for (int i = 0; i < V; ++i) ss += (double)h[i] * (double)h[i];
     }
     ss = wave_sum(ss);
     if constexpr (TPR > 64) {
@@ -222,23 +270,24 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
     for (int p = 0; p < P; ++p) {
         const int unit = p * TPR + t, c = unit * V;
         if (c >= nb * 32) continue;                       // lanes of a block go together
-        float y[V];
+        float h[V], y[V];
+        unpack(q[p], h);
         if (gain != nullptr) {
             float g[V];
-            if constexpr (V == 4) {
-                load_piece(gain + c, n - c, g);
-            } else {
-                float g0[4], g1[4];
-                load_piece(gain + c, n - c, g0);
-                load_piece(gain + c + 4, n - c - 4, g1);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { g[i] = g0[i]; g[4 + i] = g1[i]; }
+            for (int i = 0; i < V; i += 4) {
+                uint4 u = load_whole(gain, c + i, n);
+                finish_piece<RAGGED>(u, gain, c + i, n);
+                float g4[4];
+                unpack(u, g4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) g[i + k] = g4[k];
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = (float)((double)h[p][i] * f * (double)g[i]);
+            for (int i = 0; i < V; ++i) y[i] = (float)((double)h[i] * f * (double)g[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = (float)((double)h[p][i] * f);
+            for (int i = 0; i < V; ++i) y[i] = (float)((double)h[i] * f);
         }
         put_blocks<F, V>(y, unit, nb, codes + row * ldc, scales + row * lds, flags);
     }
@@ -246,40 +295,57 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 
 // Squared error of the MX quantiser and its derivative:  loss_t = (1/n) sum_i (y_i - yhat_i)^2,  dY_i = c (2/n) (y_i - yhat_i).  yhat is
 // constant around almost every y (the scale is a power of two), so this is the derivative wherever there is one.
-template <int F, bool BF16OUT>
+//
+// A workgroup takes the pieces of a row group (a long row, or rg short ones side by side) 4 x 256 at a time, or those of four groups of short rows,
+// all four under way together.
+template <int F, bool BF16OUT, bool RAGGED>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
                                                            long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
+    constexpr int U = 4;
     __shared__ double tot[4];
     Y += (long)blockIdx.y * sy;
     const float f = scale * 2.f / (float)n;
-    const int xt = w.rg > 1 ? 1 : (w.upr + 255) / 256;
+    const bool side = w.rg > 1;
+    const int r_in = side ? (int)threadIdx.x / w.upr : 0, u_in = side ? (int)threadIdx.x - r_in * w.upr : (int)threadIdx.x;
     const long groups = ((long)T + w.rg - 1) / w.rg;
+    const long row_step = side ? (long)gridDim.x * w.rg : 0, hop = side ? U * (long)gridDim.x : gridDim.x;
     double acc = 0.0;
-    for (long item = blockIdx.x; item < groups * xt; item += gridDim.x) {
-        const long group = item / xt;
-        const int r_in = w.rg > 1 ? (int)threadIdx.x / w.upr : 0;
-        const int unit = w.rg > 1 ? (int)threadIdx.x - r_in * w.upr : (int)(item - group * xt) * 256 + (int)threadIdx.x;
-        const long row = group * w.rg + r_in;
-        const int left = n - unit * 4;
-        if (r_in >= w.rg || unit >= w.upr || row >= T) continue;
-        float v[4];
-        load_piece(Y + row * ldy + (long)unit * 4, left, v);
-        const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
-        unsigned code[1];
-        mx_encode<F, 4>(v, byte, code);
-        float e[4];
-        mx_decode4<F, 0>(code[0], mx_scale(byte), e);
-        float ss = 0.f;
+    for (long group = blockIdx.x; group < groups; group += hop) {
+        for (int first = 0; first < w.upr; first += side ? w.upr : 256 * U) {
+            uint4 q[U];
+            bool in[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            e[i] = byte == 255u ? __uint_as_float(0x7fc00000u) : v[i] - e[i];
-            ss += e[i] * e[i];
-            e[i] *= f;
-        }
-        acc += (double)ss;
-        if (dYv != nullptr && left > 0) {
-            if constexpr (BF16OUT) store_piece<4>(static_cast<bf16_t*>(dYv) + (long)blockIdx.y * sdy + row * lddy + (long)unit * 4, left, e);
-            else store_piece(static_cast<float*>(dYv) + (long)blockIdx.y * sdy + row * lddy + (long)unit * 4, left, e);
+            for (int k = 0; k < U; ++k) {
+                const long row = group * w.rg + r_in + k * row_step;
+                const int unit = side ? u_in : first + k * 256 + u_in;
+                in[k] = r_in < w.rg && unit < w.upr && row < T;
+                q[k] = load_whole(Y + (in[k] ? row : 0) * ldy, in[k] ? unit * 4 : 0, n);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (!in[k]) continue;
+                const long row = group * w.rg + r_in + k * row_step;
+                const int c = 4 * (side ? u_in : first + k * 256 + u_in);
+                finish_piece<RAGGED>(q[k], Y + row * ldy, c, n);
+                float v[4], e[4];
+                unpack(q[k], v);
+                const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
+                unsigned code[1];
+                mx_encode<F, 4>(v, byte, code);
+                mx_decode4<F, 0>(code[0], mx_scale(byte), e);
+                float ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[i] = byte == 255u ? __uint_as_float(0x7fc00000u) : v[i] - e[i];
+                    ss += e[i] * e[i];
+                    e[i] *= f;
+                }
+                acc += (double)ss;
+                if (dYv != nullptr && c < n) {
+                    if constexpr (BF16OUT) store_piece<4>(static_cast<bf16_t*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
+                    else store_piece(static_cast<float*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
+                }
+            }
         }
     }
     acc = wave_sum(acc);
@@ -294,10 +360,13 @@ Walk make_walk(int n, int V) {
     w.rg = w.upr <= 128 ? 256 / w.upr : 1;
     return w;
 }
-dim3 walk_grid(const Walk& w, int T) {
+// at most 16384 workgroups, and each `batch` rows at a time where that leaves 2048, eight for every compute unit
+dim3 walk_grid(const Walk& w, int T, int batch) {
     const long groups = ((long)T + w.rg - 1) / w.rg;
     const long xt = w.rg > 1 ? 1 : (w.upr + 255) / 256;
-    long gy = 16384 / xt;
+    long gy = (groups + batch - 1) / batch;
+    if (gy * xt < 2048) gy = (2048 + xt - 1) / xt;
+    if (gy * xt > 16384) gy = 16384 / xt;
     gy = gy < 1 ? 1 : gy < groups ? gy : groups;
     return dim3((unsigned)xt, (unsigned)gy);
 }
@@ -305,9 +374,12 @@ dim3 walk_grid(const Walk& w, int T) {
 template <class IN, int F, int P, int TPR>
 hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
     constexpr int rows = 256 / TPR;
-    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR>), dim3((unsigned)(((long)m.T + rows - 1) / rows)), dim3(256), 0, s,
-                       static_cast<const IN*>(m.X), m.ldx, static_cast<const IN*>(m.res), m.ldr, static_cast<IN*>(m.H), m.ldh, m.gain, m.eps, m.T,
-                       m.n, (m.n + 31) / 32, m.codes, m.ldc, m.scales, m.lds, m.flags);
+#define DQ_GO(RAGGED)                                                                                                                              \
+    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, RAGGED>), dim3((unsigned)(((long)m.T + rows - 1) / rows)), dim3(256), 0, s,              \
+                       static_cast<const IN*>(m.X), m.ldx, static_cast<const IN*>(m.res), m.ldr, static_cast<IN*>(m.H), m.ldh, m.gain, m.eps, m.T, \
+                       m.n, (m.n + 31) / 32, m.codes, m.ldc, m.scales, m.lds, m.flags)
+    if (m.n % Piece<IN>::V != 0) DQ_GO(true); else DQ_GO(false);
+#undef DQ_GO
     return hipGetLastError();
 }
 template <class IN, int F>
@@ -335,12 +407,14 @@ hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int
     if (T < 1 || n < 1) return hipSuccess;
     const Walk w = make_walk(n, x_is_bf16 ? 8 : 4);
     const int nb = (int)((n + 31L) / 32);
-#define DQ_GO(IN, F)                                                                                                                              \
-    hipLaunchKernelGGL((mx_quantize_kernel<IN, F>), walk_grid(w, T), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, scales, \
-                       lds, w, flags)
+#define DQ_GO2(IN, F, RAGGED)                                                                                                                        \
+    hipLaunchKernelGGL((mx_quantize_kernel<IN, F, RAGGED>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, \
+                       scales, lds, w, flags)
+#define DQ_GO(IN, F) do { if (n % Piece<IN>::V != 0) DQ_GO2(IN, F, true); else DQ_GO2(IN, F, false); } while (0)
     if (x_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
 #undef DQ_GO
+#undef DQ_GO2
     return hipGetLastError();
 }
 
@@ -349,7 +423,7 @@ hipError_t launch_mx_dequantize(int format, const unsigned char* codes, long ldc
     if (T < 1 || n < 1) return hipSuccess;
     const Walk w = make_walk(n, y_is_bf16 ? 8 : 4);
 #define DQ_GO(OUT, F)                                                                                                                        \
-    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), walk_grid(w, T), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
+    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), walk_grid(w, T, 1), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
                        ldy, w)
     if (y_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
@@ -363,15 +437,24 @@ hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s) {
     return m.format == DQ_MXFP4 ? norm_shape<float, DQ_MXFP4>(m, s) : norm_shape<float, DQ_MXFP8>(m, s);
 }
 
+int mx_objective_grid(int T, int n) {
+    const Walk w = make_walk(n, 4);
+    const long groups = ((long)T + w.rg - 1) / w.rg, g = w.rg > 1 ? (groups + 3) / 4 : groups;
+    return (int)(g < 2048 ? g : 2048);
+}
+
 hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy) {
     if (batch < 1 || T < 1) return hipSuccess;
     const Walk w = make_walk(n, 4);
-#define DQ_GO(F, BF) \
-    hipLaunchKernelGGL((mx_objective_kernel<F, BF>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, stride_dy, w)
+#define DQ_GO2(F, BF, RAGGED)                                                                                                                          \
+    hipLaunchKernelGGL((mx_objective_kernel<F, BF, RAGGED>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, \
+                       stride_dy, w)
+#define DQ_GO(F, BF) do { if (n & 3) DQ_GO2(F, BF, true); else DQ_GO2(F, BF, false); } while (0)
     if (format == DQ_MXFP4) { if (dy_is_bf16) DQ_GO(DQ_MXFP4, true); else DQ_GO(DQ_MXFP4, false); }
     else { if (dy_is_bf16) DQ_GO(DQ_MXFP8, true); else DQ_GO(DQ_MXFP8, false); }
 #undef DQ_GO
+#undef DQ_GO2
     return hipGetLastError();
 }
 

@@ -340,7 +340,8 @@ hipError_t launch_rows_shape(const float* Y, long ldy, int T, int n, float scale
 
 }  // namespace
 
-int objective_grid(int T, int n) {
+int objective_grid(int objective, int T, int n) {
+    if (objective == OBJ_MXFP4 || objective == OBJ_MXFP8) return mx_objective_grid(T, n);
     const int rpw = n <= 1024 ? 4 : 1;
     long g = ((long)T + rpw - 1) / rpw;
     // measured at T = 8192..16384: rows of n > 1024 (one workgroup per row) run best with about 1024 workgroups
