@@ -122,7 +122,7 @@ def dq_mx_row_bytes(fmt: int, n: int) -> tuple[int, int]:
 
 
 def _ptr(t):
-    return 0 if t is None else int(t.data_ptr())
+    return 0 if t is None else t.data_ptr()
 
 
 def dq_whip_loss_grad_noalloc(stream, Y, reduce, loss, dY, dy_dtype):
@@ -140,8 +140,9 @@ def _ld(t):
     """Leading dimension (elements) of the last two dims of a row-major tensor."""
     if t is None:
         return 0
-    assert t.stride(-1) == 1, "matrices must be row-major with unit column stride"
-    return int(t.stride(-2))
+    s = t.stride()
+    assert s[-1] == 1, "matrices must be row-major with unit column stride"
+    return s[-2]
 
 
 class Context:
