@@ -6,6 +6,9 @@
 namespace dq {
 namespace {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
 template <class T> struct Piece;                       // what one 16-byte access holds
 template <> struct Piece<float> { static constexpr int V = 4; };
 template <> struct Piece<bf16_t> { static constexpr int V = 8; };
@@ -28,33 +31,28 @@ __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
     }
 }
 // The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  Whole pieces without a
-// branch (a piece that is none reads the row's first one instead, and is cleared); with RAGGED, n no multiple of V, the row's last piece again
-// value by value.
+// branch; a piece that is not whole reads the row's first one instead, and again value by value afterwards.
 // STREAM: past the caches, for what is read once by a kernel that writes less than it reads (quantiser 8192 x 8192 42 -> 34 us, objective 8192 x 4096
 // 39 -> 35; the norm, which writes as much, 50 -> 52).
 template <bool STREAM, class T>
 __device__ __forceinline__ uint4 load_whole(const T* row, int c, int n) {
-    typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
     if (n < Piece<T>::V) return make_uint4(0u, 0u, 0u, 0u);
     const u32x4* at = reinterpret_cast<const u32x4*>(row + (c + Piece<T>::V <= n ? c : 0));
     const u32x4 q = STREAM ? __builtin_nontemporal_load(at) : *at;
     return make_uint4(q.x, q.y, q.z, q.w);
 }
-template <bool RAGGED, class T>
+template <class T>
 __device__ __forceinline__ void finish_piece(uint4& q, const T* row, int c, int n) {
     constexpr int V = Piece<T>::V;
     if (c + V > n) {
-        q = make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (RAGGED) {
-            unsigned w[4] = {0u, 0u, 0u, 0u};
+        unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int i = 0; i < V - 1; ++i)
-                if (c + i < n) {
-                    if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
-                    else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
-                }
-            q = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int i = 0; i < V - 1; ++i)
+            if (c + i < n) {
+                if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
+                else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+            }
+        q = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 __device__ __forceinline__ void store_piece(float* dst, int left, const float (&v)[4]) {
@@ -92,20 +90,26 @@ __device__ __forceinline__ unsigned piece_top(const float (&v)[NV]) {
     return top;
 }
 
+// PAST: past the caches
+template <bool PAST, class W>
+__device__ __forceinline__ void store_words(W* at, W w) {
+    if constexpr (PAST) __builtin_nontemporal_store(w, at);
+    else *at = w;
+}
 // Codes of piece `unit` of a row (V values each) and, from the first lane of a block, its scale; the row's last block also fills the scales
 // up to a multiple of 16.
-template <int F, int NV>
+template <int F, int NV, bool PAST>
 __device__ __forceinline__ void put_blocks(const float (&v)[NV], int unit, int nb, unsigned char* codes, unsigned char* scales, unsigned* flags) {
     constexpr int LANES = 32 / NV;
     const unsigned byte = mx_scale_byte<F>(mx_group_max<LANES>(piece_top(v)));
     unsigned w[F == DQ_MXFP4 ? (NV + 7) / 8 : NV / 4];
     mx_encode<F, NV>(v, byte, w);
     if constexpr (F == DQ_MXFP4) {
-        if constexpr (NV == 8) reinterpret_cast<unsigned*>(codes)[unit] = w[0];
-        else reinterpret_cast<unsigned short*>(codes)[unit] = (unsigned short)w[0];
+        if constexpr (NV == 8) store_words<PAST>(reinterpret_cast<unsigned*>(codes) + unit, w[0]);
+        else store_words<PAST>(reinterpret_cast<unsigned short*>(codes) + unit, (unsigned short)w[0]);
     } else {
-        if constexpr (NV == 8) reinterpret_cast<uint2*>(codes)[unit] = make_uint2(w[0], w[1]);
-        else reinterpret_cast<unsigned*>(codes)[unit] = w[0];
+        if constexpr (NV == 8) store_words<PAST>(reinterpret_cast<u32x2*>(codes) + unit, u32x2{w[0], w[1]});
+        else store_words<PAST>(reinterpret_cast<unsigned*>(codes) + unit, w[0]);
     }
     if (unit % LANES == 0) {
         const int block = unit / LANES;
@@ -132,7 +136,7 @@ __device__ __forceinline__ bool walk_start(const Walk& w, int& row, int& unit) {
 }
 
 // U rows of a thread under way at a time
-template <class IN, int F, bool RAGGED>
+template <class IN, int F, bool PAST>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__ X, long ldx, int T, int n, int nb, unsigned char* __restrict__ codes,
                                                           long ldc, unsigned char* __restrict__ scales, long lds, Walk w, unsigned* flags) {
     constexpr int V = Piece<IN>::V, U = 4;
@@ -147,10 +151,10 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__
         for (int k = 0; k < U; ++k) {
             const long at = r + k * step;
             if (at >= T) break;
-            finish_piece<RAGGED>(q[k], X + at * ldx, unit * V, n);
+            finish_piece(q[k], X + at * ldx, unit * V, n);
             float v[V];
             unpack(q[k], v);
-            put_blocks<F, V>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
+            put_blocks<F, V, PAST>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
         }
     }
 }
@@ -209,7 +213,7 @@ __device__ __forceinline__ double inverse_root(double m) {
 // One token row per TPR threads, P pieces each:  h = x + res (rounded to the stored type: the norm is that of what is stored),
 // y = fp32(h / sqrt(mean h^2 + eps) * gain), then MX blocks of y.  The mean and y are formed in 64 bits and rounded once: a difference in
 // the last bit of y flips codes next to a border, and a row's sum in 32 bits moves every value of the row.  H may be X or res.
-template <class IN, int F, int P, int TPR, bool RAGGED>
+template <class IN, int F, int P, int TPR, bool PAST>
 __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx, const IN* res, long ldr, IN* H, long ldh, const float* __restrict__ gain,
                                                           float eps, int T, int n, int nb, unsigned char* __restrict__ codes, long ldc,
                                                           unsigned char* __restrict__ scales, long lds, unsigned* flags) {
@@ -227,8 +231,8 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int c = (p * TPR + t) * V;
-            finish_piece<RAGGED>(q[p], X + at * ldx, c, n);
-            finish_piece<RAGGED>(z[p], res + at * ldr, c, n);
+            finish_piece(q[p], X + at * ldx, c, n);
+            finish_piece(z[p], res + at * ldr, c, n);
             float h[V], r[V];
             unpack(q[p], h);
             unpack(z[p], r);
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
         }
     } else {
 #pragma unroll
-        for (int p = 0; p < P; ++p) finish_piece<RAGGED>(q[p], X + at * ldx, (p * TPR + t) * V, n);
+        for (int p = 0; p < P; ++p) finish_piece(q[p], X + at * ldx, (p * TPR + t) * V, n);
     }
     double ss = 0.0;
 #pragma unroll
@@ -247,8 +251,8 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
         const int c = (p * TPR + t) * V;
         if (H != nullptr && live) {
             if (c + V <= n) {
-                *reinterpret_cast<uint4*>(H + row * ldh + c) = q[p];
-            } else if (RAGGED && c < n) {
+                store_words<PAST>(reinterpret_cast<u32x4*>(H + row * ldh + c), u32x4{q[p].x, q[p].y, q[p].z, q[p].w});
+            } else if (c < n) {
                 const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
 #pragma unroll
                 for (int i = 0; i < V - 1; ++i)
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
                 uint4 u = load_whole<false>(gain, c + i, n);
-                finish_piece<RAGGED>(u, gain, c + i, n);
+                finish_piece(u, gain, c + i, n);
                 float g4[4];
                 unpack(u, g4);
 #pragma unroll
@@ -294,7 +298,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = (float)((double)h[i] * f);
         }
-        put_blocks<F, V>(y, unit, nb, codes + row * ldc, scales + row * lds, flags);
+        put_blocks<F, V, false>(y, unit, nb, codes + row * ldc, scales + row * lds, flags);
     }
 }
 
@@ -303,7 +307,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 //
 // A workgroup takes the pieces of a row group (a long row, or rg short ones side by side) 4 x 256 at a time, or those of four groups of short rows,
 // all four under way together.
-template <int F, bool BF16OUT, bool RAGGED>
+template <int F, bool BF16OUT>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
                                                            long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
     constexpr int U = 4;
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
                 if (!in[k]) continue;
                 const long row = group * w.rg + r_in + k * row_step;
                 const int c = 4 * (side ? u_in : first + k * 256 + u_in);
-                finish_piece<RAGGED>(q[k], Y + row * ldy, c, n);
+                finish_piece(q[k], Y + row * ldy, c, n);
                 float v[4], e[4];
                 unpack(q[k], v);
                 const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
@@ -376,14 +380,18 @@ dim3 walk_grid(const Walk& w, int T, int batch) {
     return dim3((unsigned)xt, (unsigned)gy);
 }
 
+// The norm's sum and the quantiser's codes leave past the caches where the input alone is more than the L2s hold (32 MB), so that little of them would be
+// found there: norm 8192 x 4096 (bf16, 67 MB) 50 -> 45 us, quantiser 8192 x 8192 34.6 -> 31.8.  Of less, what follows reads it in the caches.
+bool past_caches(int T, int n, int is_bf16) { return (long)T * n * (is_bf16 ? 2 : 4) > (32L << 20); }
+
 template <class IN, int F, int P, int TPR>
 hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
     constexpr int rows = 256 / TPR;
-#define DQ_GO(RAGGED)                                                                                                                              \
-    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, RAGGED>), dim3((unsigned)(((long)m.T + rows - 1) / rows)), dim3(256), 0, s,              \
+#define DQ_GO(PAST)                                                                                                                                \
+    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, PAST>)  , dim3((unsigned)(((long)m.T + rows - 1) / rows)), dim3(256), 0, s,              \
                        static_cast<const IN*>(m.X), m.ldx, static_cast<const IN*>(m.res), m.ldr, static_cast<IN*>(m.H), m.ldh, m.gain, m.eps, m.T, \
                        m.n, (m.n + 31) / 32, m.codes, m.ldc, m.scales, m.lds, m.flags)
-    if (m.n % Piece<IN>::V != 0) DQ_GO(true); else DQ_GO(false);
+    if (past_caches(m.T, m.n, m.x_is_bf16)) DQ_GO(true); else DQ_GO(false);
 #undef DQ_GO
     return hipGetLastError();
 }
@@ -412,10 +420,10 @@ hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int
     if (T < 1 || n < 1) return hipSuccess;
     const Walk w = make_walk(n, x_is_bf16 ? 8 : 4);
     const int nb = (int)((n + 31L) / 32);
-#define DQ_GO2(IN, F, RAGGED)                                                                                                                        \
-    hipLaunchKernelGGL((mx_quantize_kernel<IN, F, RAGGED>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, \
+#define DQ_GO2(IN, F, PAST)                                                                                                                        \
+    hipLaunchKernelGGL((mx_quantize_kernel<IN, F, PAST>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, \
                        scales, lds, w, flags)
-#define DQ_GO(IN, F) do { if (n % Piece<IN>::V != 0) DQ_GO2(IN, F, true); else DQ_GO2(IN, F, false); } while (0)
+#define DQ_GO(IN, F) do { if (past_caches(T, n, x_is_bf16)) DQ_GO2(IN, F, true); else DQ_GO2(IN, F, false); } while (0)
     if (x_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
 #undef DQ_GO
@@ -452,14 +460,11 @@ hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int 
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy) {
     if (batch < 1 || T < 1) return hipSuccess;
     const Walk w = make_walk(n, 4);
-#define DQ_GO2(F, BF, RAGGED)                                                                                                                          \
-    hipLaunchKernelGGL((mx_objective_kernel<F, BF, RAGGED>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, \
-                       stride_dy, w)
-#define DQ_GO(F, BF) do { if (n & 3) DQ_GO2(F, BF, true); else DQ_GO2(F, BF, false); } while (0)
+#define DQ_GO(F, BF) \
+    hipLaunchKernelGGL((mx_objective_kernel<F, BF>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, stride_dy, w)
     if (format == DQ_MXFP4) { if (dy_is_bf16) DQ_GO(DQ_MXFP4, true); else DQ_GO(DQ_MXFP4, false); }
     else { if (dy_is_bf16) DQ_GO(DQ_MXFP8, true); else DQ_GO(DQ_MXFP8, false); }
 #undef DQ_GO
-#undef DQ_GO2
     return hipGetLastError();
 }
 
