@@ -561,6 +561,7 @@ hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
 //   64 x 32 tiles, 4 groups against 64 x 64, 2      128 x 4096, 4096: 5.7, 6.6;  256 x 4096, 4096 (512 and 256 workgroups): 11.1, 7.2
 //   64 x 64 tiles against 128 x 64, 2 groups        256 x 4096, 4096: 7.2, 8.7;  512 x 4096, 4096 (512 and 256 workgroups): 11.4, 9.8
 //   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 9.8, 11.4;  1024 x 4096, 4096: 18.7, 14.7
+//   128 x 128 tiles, four stages in LDS against two   operands not in the L2s: 1024 x 4096, 4096 (256 workgroups): 17.1, 22.1;  2048 x 4096, 4096 (512): 32.5, 29.3
 //   128 x 128 tiles against 256 x 256               2048 x 4096, 4096 (512 and 128 workgroups): 25.4, 26.5
 // that is, the largest tile that still gives most compute units a workgroup.  A kernel of no work takes 2 us, one of 64 in the reduction 4 to 5.
 template <int FA, int FB, class OUT>
@@ -579,7 +580,8 @@ hipError_t launch_types(const GemmMx& g, hipStream_t s) {
         if constexpr (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8, 1, 160>(g, s);
         else if constexpr (!exact) return launch_tile<FA, FB, OUT, 4, 4, 4, 1, 160>(g, s);
     }
-    if (tiles(128, 128) >= most) return launch_tile<FA, FB, OUT, 2, 2, 4, 1, 80>(g, s);
+    if (tiles(128, 128) > 256) return launch_tile<FA, FB, OUT, 2, 2, 4, 1, 80>(g, s);         // two workgroups a compute unit
+    if (tiles(128, 128) >= most) return launch_tile<FA, FB, OUT, 2, 2, 4, 1, 160>(g, s);
     if (tiles(128, 64) >= most) return launch_tile<FA, FB, OUT, 2, 1, 4, 2, 160>(g, s);
     if (tiles(64, 64) >= most) return launch_tile<FA, FB, OUT, 1, 1, 4, 2, 80>(g, s);
     return launch_tile<FA, FB, OUT, 1, 1, 2, 4, 160>(g, s);
