@@ -136,6 +136,31 @@ def test_read_every_code(ctx):
             assert torch.equal(torch.nan_to_num(Y.cpu(), nan=12345.0), torch.nan_to_num(ref.float().to(dtype), nan=12345.0))
 
 
+@pytest.mark.parametrize("xdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_large_inputs_give_the_codes_of_their_parts(ctx, fmt, xdt):
+    """More than the caches hold takes kernels of its own; the rows in parts take those that the oracle has checked."""
+    T, n = 4500, 4001 if xdt == B.DQ_BF16 else 3001
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    X, res, H, H2 = (torch.empty((T, up(n, 8)), dtype=TYPES[xdt], device="cuda")[:, :n] for _ in range(4))
+    X.copy_(torch.randn((T, n), device="cuda", generator=g))
+    res.copy_(torch.randn((T, n), device="cuda", generator=g))
+    assert T * n * X.element_size() > 32 << 20 > 1500 * n * X.element_size()
+    gain = torch.rand(n, device="cuda", generator=g)
+    for norm in (False, True):
+        whole, parts = stored(T, n, fmt), stored(T, n, fmt)
+        for out, h, bounds in ((whole, H, [(0, T)]), (parts, H2, [(0, 1500), (1500, 3000), (3000, T)])):
+            for lo, hi in bounds:
+                c, s = out[0][lo:hi], out[1][lo:hi]
+                if norm:
+                    ctx.dq_mx_rms_norm(X[lo:hi], xdt, res[lo:hi], h[lo:hi], gain, 1e-5, fmt, c, s)
+                else:
+                    ctx.dq_mx_quantize(X[lo:hi], xdt, fmt, c, s)
+        assert torch.equal(whole[0], parts[0]) and torch.equal(whole[1], parts[1])
+    assert torch.equal(H, H2)
+
+
 # ----------------------------------------------------------------------------------- norm
 NORM_SHAPES = [(1, 1), (3, 33), (130, 40), (5, 300), (4, 512), (9, 513), (6, 1000), (3, 1024), (5, 2048), (2, 2890), (1, 4096), (7, 4100), (3, 8192), (0, 64)]
 
@@ -218,6 +243,21 @@ def test_rms_norm_of_rows_that_are_not_finite(ctx):
 
 
 # ----------------------------------------------------------------------------------- objective
+def test_objective_of_many_rows_and_of_many_problems(ctx):
+    """More rows than the workgroups of a launch take at once, long and short ones, and so many problems that each gets few workgroups."""
+    for b, T, n, some in ((1, 5000, 1201, [0]), (1, 300000, 33, [0]), (20000, 5, 600, [0, 1, 9999, 19999])):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(n)
+        Y = torch.empty((b, T, up(n, 4)), device="cuda")[:, :, :n]
+        Y.copy_(torch.randn((b, T, n), device="cuda", generator=g))
+        dY, loss = torch.empty((b, T, up(n, 4)), device="cuda")[:, :, :n], torch.empty(b, device="cuda")
+        ctx.dq_objective_loss_grad(B.DQ_OBJ_MXFP8, 4, Y, B.DQ_REDUCE_TOKEN_MEAN, loss, dY, B.DQ_F32)
+        for i in some:
+            ref_loss, ref = mx.objective(Y[i].cpu().numpy(), B.DQ_MXFP8, "mean")
+            assert (np.abs(dY[i].double().cpu().numpy() - ref) <= np.abs(ref) * 4 * 2.0 ** -24).all()
+            assert abs(loss[i].item() - ref_loss) <= 8 * 2.0 ** -24 * ref_loss
+
+
 @pytest.mark.parametrize("b,T,n", [(1, 1, 1), (1, 5, 33), (3, 45, 640), (1, 37, 101), (64, 9, 128), (2, 300, 80), (1, 19, 1500), (1, 9, 4096), (1, 5, 8192), (1, 7, 5001)])
 @pytest.mark.parametrize("grad", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -311,15 +351,59 @@ def test_gemm_mx(ctx, fa, fb, cdt, M, N, K):
     assert torch.equal(C, again)
 
 
+# Shapes that are multiples of no tile, for each kernel that the size of the result chooses (256, 128 with more and with fewer workgroups than compute
+# units, 128 x 64, 64, 64 x 32, up to 16 rows with a long reduction), with reductions of one block, of odd counts of stages and of pieces of 512
+@pytest.mark.parametrize("M,N", [(3601, 3570), (2049, 2190), (1701, 1750), (1000, 1601), (801, 1000), (200, 333), (9, 700)])
+@pytest.mark.parametrize("K", [20, 545, 1700, 5200])
 @pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (0, 1), (1, 1)])
-@pytest.mark.parametrize("M,N,K", [(5, 40, 600), (300, 280, 600)])
+def test_gemm_mx_every_kernel(ctx, fa, fb, cdt, M, N, K):
+    _, A, As = random_matrix(M, K, fa, 41 * M + K)
+    _, Bm, Bs = random_matrix(N, K, fb, 43 * N + K)
+    vals = []
+    for rows, fmt, c, s in ((M, fa, A, As), (N, fb, Bm, Bs)):          # read back by the library: that is tested above
+        Y = torch.empty((rows, up(K, 8)), device="cuda")[:, :K]
+        ctx.dq_mx_dequantize(fmt, c, s, Y, B.DQ_F32)
+        vals.append(Y.double())
+    buf, C = view(M, N, up(N, 8) + 8, TYPES[cdt], 7.0)
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, C, cdt)
+    ref = vals[0] @ vals[1].t().contiguous()
+    s = vals[0].abs() @ vals[1].abs().t().contiguous()
+    tol = s * (4 * -(-K // 128) + 16) * 2.0 ** -23 + 1e-38              # as product_bound
+    if cdt == B.DQ_BF16:
+        tol += ref.abs() * 2.0 ** -8 + (s * 2.0 ** -11 if B.DQ_MXFP8 in (fa, fb) else 0.0)
+    assert bool(((C.double() - ref).abs() <= tol).all())
+    assert (buf[:, N:] == 7.0).all()
+    again = torch.empty_like(buf)[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, again, cdt)
+    assert torch.equal(C, again)
+
+
+@pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (1, 1)])
+def test_gemm_of_rows_far_apart(ctx, fa, fb):
+    """Rows of A, then of B, 8 MiB apart and more: beyond what the tiles address."""
+    M, N, K, far = 70, 50, 700, (1 << 23) + 64
+    a, A, As = random_matrix(M, K, fa, 91)
+    b, Bm, Bs = random_matrix(N, K, fb, 92)
+    ref = a @ b.T
+    for spread in ("a", "b"):
+        src = A if spread == "a" else Bm
+        wide = torch.empty((src.shape[0], far), dtype=torch.uint8, device="cuda")[:, :src.shape[1]]
+        wide.copy_(src)
+        C = torch.empty((M, up(N, 8)), device="cuda")[:, :N]
+        ctx.dq_gemm_mx(M, N, K, fa, wide if spread == "a" else A, As, fb, wide if spread == "b" else Bm, Bs, C, B.DQ_F32)
+        assert (np.abs(C.double().cpu().numpy() - ref) <= product_bound(a, b, ref, K, fa, fb, B.DQ_F32)).all()
+
+
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (0, 1), (1, 1)])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 600), (300, 280, 600), (1000, 1601, 600), (1701, 1750, 600), (3601, 3570, 600)])
 def test_gemm_of_blocks_that_are_nan(ctx, M, N, K, fa, fb, cdt):
     a, A, As = random_matrix(M, K, fa, 71)
     b, Bm, Bs = random_matrix(N, K, fb, 72)
     As[3, 18] = 255                                            # the last block, cut short
     Bs[N - 2, 0] = 255
-    C = torch.zeros((M, N), device="cuda", dtype=TYPES[cdt])
+    C = torch.zeros((M, up(N, 8)), device="cuda", dtype=TYPES[cdt])[:, :N]
     ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, C, cdt)
     bad = torch.isnan(C).cpu().numpy()
     want = np.zeros((M, N), dtype=bool)
