@@ -90,26 +90,20 @@ __device__ __forceinline__ unsigned piece_top(const float (&v)[NV]) {
     return top;
 }
 
-// PAST: past the caches
-template <bool PAST, class W>
-__device__ __forceinline__ void store_words(W* at, W w) {
-    if constexpr (PAST) __builtin_nontemporal_store(w, at);
-    else *at = w;
-}
 // Codes of piece `unit` of a row (V values each) and, from the first lane of a block, its scale; the row's last block also fills the scales
 // up to a multiple of 16.
-template <int F, int NV, bool PAST>
+template <int F, int NV>
 __device__ __forceinline__ void put_blocks(const float (&v)[NV], int unit, int nb, unsigned char* codes, unsigned char* scales, unsigned* flags) {
     constexpr int LANES = 32 / NV;
     const unsigned byte = mx_scale_byte<F>(mx_group_max<LANES>(piece_top(v)));
     unsigned w[F == DQ_MXFP4 ? (NV + 7) / 8 : NV / 4];
     mx_encode<F, NV>(v, byte, w);
     if constexpr (F == DQ_MXFP4) {
-        if constexpr (NV == 8) store_words<PAST>(reinterpret_cast<unsigned*>(codes) + unit, w[0]);
-        else store_words<PAST>(reinterpret_cast<unsigned short*>(codes) + unit, (unsigned short)w[0]);
+        if constexpr (NV == 8) reinterpret_cast<unsigned*>(codes)[unit] = w[0];
+        else reinterpret_cast<unsigned short*>(codes)[unit] = (unsigned short)w[0];
     } else {
-        if constexpr (NV == 8) store_words<PAST>(reinterpret_cast<u32x2*>(codes) + unit, u32x2{w[0], w[1]});
-        else store_words<PAST>(reinterpret_cast<unsigned*>(codes) + unit, w[0]);
+        if constexpr (NV == 8) reinterpret_cast<uint2*>(codes)[unit] = make_uint2(w[0], w[1]);
+        else reinterpret_cast<unsigned*>(codes)[unit] = w[0];
     }
     if (unit % LANES == 0) {
         const int block = unit / LANES;
@@ -136,7 +130,7 @@ __device__ __forceinline__ bool walk_start(const Walk& w, int& row, int& unit) {
 }
 
 // U rows of a thread under way at a time
-template <class IN, int F, bool PAST>
+template <class IN, int F>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__ X, long ldx, int T, int n, int nb, unsigned char* __restrict__ codes,
                                                           long ldc, unsigned char* __restrict__ scales, long lds, Walk w, unsigned* flags) {
     constexpr int V = Piece<IN>::V, U = 4;
@@ -154,7 +148,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__
             finish_piece(q[k], X + at * ldx, unit * V, n);
             float v[V];
             unpack(q[k], v);
-            put_blocks<F, V, PAST>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
+            put_blocks<F, V>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
         }
     }
 }
@@ -213,6 +207,13 @@ __device__ __forceinline__ double inverse_root(double m) {
 // One token row per TPR threads, P pieces each:  h = x + res (rounded to the stored type: the norm is that of what is stored),
 // y = fp32(h / sqrt(mean h^2 + eps) * gain), then MX blocks of y.  The mean and y are formed in 64 bits and rounded once: a difference in
 // the last bit of y flips codes next to a border, and a row's sum in 32 bits moves every value of the row.  H may be X or res.
+template <bool PAST, class T>
+__device__ __forceinline__ void store_sum(T* to, const uint4& q) {
+    const u32x4 w = {q.x, q.y, q.z, q.w};
+    if constexpr (PAST) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(to));
+    else *reinterpret_cast<u32x4*>(to) = w;
+}
+
 template <class IN, int F, int P, int TPR, bool PAST>
 __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx, const IN* res, long ldr, IN* H, long ldh, const float* __restrict__ gain,
                                                           float eps, int T, int n, int nb, unsigned char* __restrict__ codes, long ldc,
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
         const int c = (p * TPR + t) * V;
         if (H != nullptr && live) {
             if (c + V <= n) {
-                store_words<PAST>(reinterpret_cast<u32x4*>(H + row * ldh + c), u32x4{q[p].x, q[p].y, q[p].z, q[p].w});
+                store_sum<PAST>(H + row * ldh + c, q[p]);
             } else if (c < n) {
                 const unsigned w[4] = {q[p].x, q[p].y, q[p].z, q[p].w};
 #pragma unroll
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = (float)((double)h[i] * f);
         }
-        put_blocks<F, V, false>(y, unit, nb, codes + row * ldc, scales + row * lds, flags);
+        put_blocks<F, V>(y, unit, nb, codes + row * ldc, scales + row * lds, flags);
     }
 }
 
@@ -380,8 +381,9 @@ dim3 walk_grid(const Walk& w, int T, int batch) {
     return dim3((unsigned)xt, (unsigned)gy);
 }
 
-// The norm's sum and the quantiser's codes leave past the caches where the input alone is more than the L2s hold (32 MB), so that little of them would be
-// found there: norm 8192 x 4096 (bf16, 67 MB) 50 -> 45 us, quantiser 8192 x 8192 34.6 -> 31.8.  Of less, what follows reads it in the caches.
+// The norm's sum leaves past the caches where the input alone is more than the L2s hold (32 MB), so that little of it would be found there when it is
+// next wanted, behind a layer: 8192 x 4096 (bf16, 67 MB) 50 -> 45 us.  Of less, and of all codes, what follows reads them in the caches (the quantiser
+// itself gains 34 -> 32 us at 8192 x 8192 by codes past them, and what reads those next loses 7).
 bool past_caches(int T, int n, int is_bf16) { return (long)T * n * (is_bf16 ? 2 : 4) > (32L << 20); }
 
 template <class IN, int F, int P, int TPR>
@@ -420,14 +422,12 @@ hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int
     if (T < 1 || n < 1) return hipSuccess;
     const Walk w = make_walk(n, x_is_bf16 ? 8 : 4);
     const int nb = (int)((n + 31L) / 32);
-#define DQ_GO2(IN, F, PAST)                                                                                                                        \
-    hipLaunchKernelGGL((mx_quantize_kernel<IN, F, PAST>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, \
-                       scales, lds, w, flags)
-#define DQ_GO(IN, F) do { if (past_caches(T, n, x_is_bf16)) DQ_GO2(IN, F, true); else DQ_GO2(IN, F, false); } while (0)
+#define DQ_GO(IN, F)                                                                                                                                    \
+    hipLaunchKernelGGL((mx_quantize_kernel<IN, F>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, scales, lds, \
+                       w, flags)
     if (x_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
 #undef DQ_GO
-#undef DQ_GO2
     return hipGetLastError();
 }
 
