@@ -353,7 +353,7 @@ dq_status dq_gemm_bf16(dq_ctx* ctx, int M, int N, int K,
 dq_status dq_mx_row_bytes(dq_mx_format format, int n, size_t* codes, size_t* scales);
 
 /* X (T x n, fp32 or bf16) -> codes and scales (out), and back: Y (T x n) = the values they stand for, rounded to the type of Y (only values below
- * 2^-126 are rounded).  T = 0 is a no-op; n is not limited.  dq_mx_quantize needs a workspace for the status word alone. */
+ * 2^-126 are rounded).  T = 0 is a no-op; T and n up to 2^31 - 1024 (DQ_ERR_UNSUPPORTED).  dq_mx_quantize needs a workspace for the status word alone. */
 dq_status dq_mx_quantize(dq_ctx* ctx, int T, int n, const void* X, dq_dtype xdt, long ldx,
                          dq_mx_format format, void* codes, long ldc, void* scales, long lds);
 dq_status dq_mx_dequantize(dq_ctx* ctx, int T, int n, dq_mx_format format, const void* codes, long ldc,
@@ -373,7 +373,7 @@ dq_status dq_mx_rms_norm(dq_ctx* ctx, int T, int n, const void* X, dq_dtype xdt,
  * product of a linear layer.  fp32 accumulation, one rounding to a bf16 C.  With a bf16 C, products of 8-bit codes run on the matrix cores'
  * 8-bit path, which sums eight products at a time to about 14 bits (an error below 1e-4 of C's norm, against the 2^-9 of its own rounding); with an
  * fp32 C they are summed in fp32.  A block whose scale is 255 makes its row of C (A) or column (B) NaN.
- * M = 0 or N = 0 is a no-op; K >= 1.  No workspace. */
+ * M = 0 or N = 0 is a no-op; K >= 1; M and N up to 2^26, K up to 2^31 - 1024 (DQ_ERR_UNSUPPORTED).  No workspace; a call gives the same bits every time. */
 dq_status dq_gemm_mx(dq_ctx* ctx, int M, int N, int K, dq_mx_format fa, const void* A, long lda,
                      const void* A_scales, long ldas, dq_mx_format fb, const void* B, long ldb,
                      const void* B_scales, long ldbs, void* C, dq_dtype cdt, long ldc);

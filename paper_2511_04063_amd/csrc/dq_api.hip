@@ -242,6 +242,8 @@ dq_status check_bytes(const void* p, long ld, long row) {
     if (!aligned16(p) || (ld & 15) != 0) return DQ_ERR_ALIGN;
     return DQ_OK;
 }
+// what the kernels count up to fits an int; a product's 16-row strips, one a workgroup, fit one launch
+constexpr int kMxMost = 0x7fffffff - 1023, kMxMostRows = 1 << 26;
 dq_status check_mx(dq_mx_format f, int n, const void* codes, long ldc, const void* scales, long lds) {
     if (!known_format(f)) return DQ_ERR_DTYPE;
     const dq_status st = check_bytes(codes, ldc, mx_code_bytes(f, n));
@@ -2311,6 +2313,7 @@ dq_status dq_mx_quantize(dq_ctx* c, int T, int n, const void* X, dq_dtype xdt, l
                          long lds) {
     if (c == nullptr) return DQ_ERR_NULL;
     if (T < 0 || n < 1) return DQ_ERR_SHAPE;
+    if (T > kMxMost || n > kMxMost) return DQ_ERR_UNSUPPORTED;
     if (T == 0) return DQ_OK;
     DQ_TRY(check_x(X, xdt, ldx, n));
     DQ_TRY(check_mx(format, n, codes, ldc, scales, lds));
@@ -2328,6 +2331,7 @@ dq_status dq_mx_dequantize(dq_ctx* c, int T, int n, dq_mx_format format, const v
                            dq_dtype ydt, long ldy) {
     if (c == nullptr) return DQ_ERR_NULL;
     if (T < 0 || n < 1) return DQ_ERR_SHAPE;
+    if (T > kMxMost || n > kMxMost) return DQ_ERR_UNSUPPORTED;
     if (T == 0) return DQ_OK;
     DQ_TRY(check_mx(format, n, codes, ldc, scales, lds));
     DQ_TRY(check_x(Y, ydt, ldy, n));
@@ -2344,6 +2348,7 @@ dq_status dq_mx_rms_norm(dq_ctx* c, int T, int n, const void* X, dq_dtype xdt, l
                          const float* gain, float eps, dq_mx_format format, void* codes, long ldc, void* scales, long lds) {
     if (c == nullptr) return DQ_ERR_NULL;
     if (T < 0) return DQ_ERR_SHAPE;
+    if (T > kMxMost) return DQ_ERR_UNSUPPORTED;
     DQ_TRY(check_n(n));
     if (!(eps >= 0.f) || eps > 3.0e38f) return DQ_ERR_SHAPE;
     if (T == 0) return DQ_OK;
@@ -2372,6 +2377,7 @@ dq_status dq_gemm_mx(dq_ctx* c, int M, int N, int K, dq_mx_format fa, const void
                      const void* B, long ldb, const void* B_scales, long ldbs, void* C, dq_dtype cdt, long ldc) {
     if (c == nullptr) return DQ_ERR_NULL;
     if (M < 0 || N < 0 || K < 1) return DQ_ERR_SHAPE;
+    if (M > kMxMostRows || N > kMxMostRows || K > kMxMost) return DQ_ERR_UNSUPPORTED;
     if (!known_format(fa) || !known_format(fb)) return DQ_ERR_DTYPE;
     if (M == 0 || N == 0) return DQ_OK;
     DQ_TRY(check_mx(fa, K, A, lda, A_scales, ldas));

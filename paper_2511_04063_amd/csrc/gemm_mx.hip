@@ -56,6 +56,7 @@ __device__ __forceinline__ Codes<F> load_codes(const unsigned char* row, int ste
     }
     return c;
 }
+
 // codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale, in bf16
 template <int F, int J>
 __device__ __forceinline__ bf16x8 values8(const Codes<F>& c, unsigned byte) {
@@ -166,9 +167,20 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles
 template <int FA, int FB, class OUT, int NT>
 hipError_t launch_direct(const GemmMx& g, hipStream_t s) {
     const long tn = (g.N + 16L * NT - 1) / (16 * NT), tm = (g.M + 15L) / 16;
-    if (tm * tn > 0x7fffffffL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, NT>), dim3((unsigned)(tm * tn)), dim3(512), 0, s, g, (int)tn);
-    return hipGetLastError();
+    // a launch counts its threads in 32 bits: 2^31 of them at a time
+    const long band = tn < (1L << 22) ? (1L << 22) / tn : 1;
+    for (long first = 0; first < tm; first += band) {
+        const long strips = tm - first < band ? tm - first : band, row = 16 * first;
+        GemmMx p = g;
+        p.A = g.A + row * g.lda;
+        p.As = g.As + row * g.ldas;
+        p.C = static_cast<OUT*>(g.C) + row * g.ldc;
+        p.M = (int)(g.M - row < 16 * strips ? g.M - row : 16 * strips);
+        hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, NT>), dim3((unsigned)(strips * tn)), dim3(512), 0, s, p, (int)tn);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ---- tiles through LDS: a workgroup of 2 x 2 wavefronts makes 64 MI x 64 NI of C, a wavefront 32 MI x 32 NI of it in 32 x 32 x 64 instructions

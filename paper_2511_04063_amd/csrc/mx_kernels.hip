@@ -204,9 +204,6 @@ __device__ __forceinline__ double inverse_root(double m) {
     return r * (1.5 - 0.5 * m * r * r);
 }
 
-// One token row per TPR threads, P pieces each:  h = x + res (rounded to the stored type: the norm is that of what is stored),
-// y = fp32(h / sqrt(mean h^2 + eps) * gain), then MX blocks of y.  The mean and y are formed in 64 bits and rounded once: a difference in
-// the last bit of y flips codes next to a border, and a row's sum in 32 bits moves every value of the row.  H may be X or res.
 template <bool PAST, class T>
 __device__ __forceinline__ void store_sum(T* to, const uint4& q) {
     const u32x4 w = {q.x, q.y, q.z, q.w};
@@ -214,6 +211,9 @@ __device__ __forceinline__ void store_sum(T* to, const uint4& q) {
     else *reinterpret_cast<u32x4*>(to) = w;
 }
 
+// One token row per TPR threads, P pieces each:  h = x + res (rounded to the stored type: the norm is that of what is stored),
+// y = fp32(h / sqrt(mean h^2 + eps) * gain), then MX blocks of y.  The mean and y are formed in 64 bits and rounded once: a difference in
+// the last bit of y flips codes next to a border, and a row's sum in 32 bits moves every value of the row.  H may be X or res.
 template <class IN, int F, int P, int TPR, bool PAST>
 __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx, const IN* res, long ldr, IN* H, long ldh, const float* __restrict__ gain,
                                                           float eps, int T, int n, int nb, unsigned char* __restrict__ codes, long ldc,
@@ -388,14 +388,23 @@ bool past_caches(int T, int n, int is_bf16) { return (long)T * n * (is_bf16 ? 2 
 
 template <class IN, int F, int P, int TPR>
 hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
-    constexpr int rows = 256 / TPR;
-#define DQ_GO(PAST)                                                                                                                                \
-    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, PAST>)  , dim3((unsigned)(((long)m.T + rows - 1) / rows)), dim3(256), 0, s,              \
-                       static_cast<const IN*>(m.X), m.ldx, static_cast<const IN*>(m.res), m.ldr, static_cast<IN*>(m.H), m.ldh, m.gain, m.eps, m.T, \
-                       m.n, (m.n + 31) / 32, m.codes, m.ldc, m.scales, m.lds, m.flags)
-    if (past_caches(m.T, m.n, m.x_is_bf16)) DQ_GO(true); else DQ_GO(false);
+    constexpr int ROWS = 256 / TPR;
+    const bool past = past_caches(m.T, m.n, m.x_is_bf16);
+    // a launch counts its threads in 32 bits: 2^30 of them at a time
+    for (long first = 0; first < m.T; first += (1L << 22) * ROWS) {
+        const long left = m.T - first, rows = left < (1L << 22) * ROWS ? left : (1L << 22) * ROWS;
+        const IN *X = static_cast<const IN*>(m.X) + first * m.ldx, *res = m.res != nullptr ? static_cast<const IN*>(m.res) + first * m.ldr : nullptr;
+        IN* H = m.H != nullptr ? static_cast<IN*>(m.H) + first * m.ldh : nullptr;
+#define DQ_GO(PAST)                                                                                                                          \
+    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, PAST>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), 0, s, X, m.ldx, res, \
+                       m.ldr, H, m.ldh, m.gain, m.eps, (int)rows, m.n, (m.n + 31) / 32, m.codes + first * m.ldc, m.ldc,                       \
+                       m.scales + first * m.lds, m.lds, m.flags)
+        if (past) DQ_GO(true); else DQ_GO(false);
 #undef DQ_GO
-    return hipGetLastError();
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 template <class IN, int F>
 hipError_t norm_shape(const MxNorm& m, hipStream_t s) {

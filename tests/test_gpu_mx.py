@@ -467,6 +467,36 @@ def test_offsets_beyond_32_bits(ctx):
     assert torch.equal(cbuf[:, :48], near[0]) and torch.equal(out[1], near[1])
 
 
+def test_more_workgroups_than_one_launch_holds(ctx):
+    """Calls whose threads would pass 2^32 go in several launches: the norm's 2^22 rows of one workgroup each, the 2^22 strips of a product of rows
+    far apart.  Rows repeat every 1024, so every launch has to give what the first one gave."""
+    T, n, fmt = (1 << 22) + 1029, 1032, B.DQ_MXFP4
+    base = torch.randn((1024, n), device="cuda").bfloat16()
+    X = base.repeat(T // 1024 + 1, 1)[:T]
+    out, ref = stored(T, n, fmt), stored(1024, n, fmt)
+    ctx.dq_mx_rms_norm(X, B.DQ_BF16, X, X, None, 1e-5, fmt, *out)
+    H = torch.empty_like(base)
+    ctx.dq_mx_rms_norm(base, B.DQ_BF16, base, H, None, 1e-5, fmt, *ref)
+    for got, want in ((out[0], ref[0]), (out[1], ref[1]), (X, H)):
+        whole = T // 1024 * 1024
+        assert (got[:whole].view(-1, 1024, got.shape[1]) == want).all() and torch.equal(got[whole:], want[:T - whole])
+    del X, out, got
+    M, N, K = (1 << 25) + 1029, 17, 40
+    a, A, As = random_matrix(1024, K, fmt, 93)
+    b, Bm, Bs = random_matrix(N, K, fmt, 94)
+    far = torch.empty((N, (1 << 23) + 64), dtype=torch.uint8, device="cuda")[:, :Bm.shape[1]]
+    far.copy_(Bm)
+    many = [t.repeat(M // 1024 + 1, 1)[:M] for t in (A, As)]
+    C = torch.empty((M, 24), dtype=torch.bfloat16, device="cuda")[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fmt, *many, fmt, far, Bs, C, B.DQ_BF16)
+    one = torch.empty((1024, 24), dtype=torch.bfloat16, device="cuda")[:, :N]
+    ctx.dq_gemm_mx(1024, N, K, fmt, A, As, fmt, far, Bs, one, B.DQ_BF16)
+    ref = a @ b.T
+    assert (np.abs(one.double().cpu().numpy() - ref) <= product_bound(a, b, ref, K, fmt, fmt, B.DQ_BF16)).all()
+    whole = M // 1024 * 1024
+    assert (C[:whole].unflatten(0, (-1, 1024)) == one).all() and torch.equal(C[whole:], one[:M - whole])
+
+
 def layer(c, X, res, H, weights, fmt, bufs, Y):
     """What a linear layer of a rotated model does with its input."""
     c.dq_mx_rms_norm(X, B.DQ_BF16, res, H, None, 1e-5, fmt, *bufs)

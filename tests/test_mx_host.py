@@ -22,6 +22,7 @@ def ctx():
     return ctypes.c_void_p(ctypes.addressof(store)), store
 
 
+MOST = 2 ** 31 - 1024
 P, Q, ODD = 1 << 20, 1 << 21, (1 << 20) + 8            # never dereferenced
 
 
@@ -52,6 +53,10 @@ def test_quantize_refuses(lib, ctx):
                           (B.DQ_ERR_ALIGN, dict(lds=24)), (B.DQ_ERR_ALIGN, dict(xdt=B.DQ_BF16, ldx=44))]:
         assert call(*changed(ok, **wrong)) == status, wrong
     assert call(*changed(ok, T=0, X=None)) == B.DQ_OK
+    far = dict(ldx=2 ** 32, ldc=2 ** 32, lds=2 ** 32)
+    for size in ("T", "n"):
+        assert call(*changed(ok, **far, **{size: MOST})) == B.DQ_ERR_WORKSPACE
+        assert call(*changed(ok, **far, **{size: MOST + 1})) == B.DQ_ERR_UNSUPPORTED
 
 
 def test_dequantize_refuses(lib, ctx):
@@ -63,6 +68,8 @@ def test_dequantize_refuses(lib, ctx):
                           (B.DQ_ERR_ALIGN, dict(codes=ODD)), (B.DQ_ERR_ALIGN, dict(ldy=42)), (B.DQ_ERR_ALIGN, dict(ydt=B.DQ_BF16, ldy=44))]:
         assert lib.dq_mx_dequantize(*changed(ok, **wrong)) == status, wrong
     assert lib.dq_mx_dequantize(*changed(ok, T=0, Y=None)) == B.DQ_OK
+    for size in ("T", "n"):
+        assert lib.dq_mx_dequantize(*changed(ok, **{size: MOST + 1})) == B.DQ_ERR_UNSUPPORTED
 
 
 def test_rms_norm_refuses(lib, ctx):
@@ -74,7 +81,7 @@ def test_rms_norm_refuses(lib, ctx):
     assert call(*changed(ok, H=P)) == B.DQ_ERR_WORKSPACE and call(*changed(ok, H=Q, ldh=48)) == B.DQ_ERR_WORKSPACE
     for status, wrong in [(B.DQ_ERR_NULL, dict(ctx=None)), (B.DQ_ERR_NULL, dict(X=None)), (B.DQ_ERR_NULL, dict(codes=None)),
                           (B.DQ_ERR_NULL, dict(scales=None)), (B.DQ_ERR_SHAPE, dict(T=-1)), (B.DQ_ERR_SHAPE, dict(n=0)),
-                          (B.DQ_ERR_UNSUPPORTED, dict(n=B.DQ_MAX_N + 1)), (B.DQ_ERR_SHAPE, dict(eps=-1e-6)), (B.DQ_ERR_SHAPE, dict(eps=float("nan"))),
+                          (B.DQ_ERR_UNSUPPORTED, dict(n=B.DQ_MAX_N + 1)), (B.DQ_ERR_UNSUPPORTED, dict(T=MOST + 1)), (B.DQ_ERR_SHAPE, dict(eps=-1e-6)), (B.DQ_ERR_SHAPE, dict(eps=float("nan"))),
                           (B.DQ_ERR_SHAPE, dict(eps=float("inf"))), (B.DQ_ERR_SHAPE, dict(ldr=32)), (B.DQ_ERR_SHAPE, dict(ldh=32)),
                           (B.DQ_ERR_SHAPE, dict(H=Q, ldh=40)), (B.DQ_ERR_SHAPE, dict(H=P, ldh=48)), (B.DQ_ERR_SHAPE, dict(ldc=32)),
                           (B.DQ_ERR_DTYPE, dict(xdt=2)), (B.DQ_ERR_DTYPE, dict(fmt=2)), (B.DQ_ERR_ALIGN, dict(res=ODD)), (B.DQ_ERR_ALIGN, dict(H=ODD)),
@@ -93,6 +100,8 @@ def test_gemm_refuses(lib, ctx):
                           (B.DQ_ERR_DTYPE, dict(cdt=2)), (B.DQ_ERR_ALIGN, dict(A=ODD)), (B.DQ_ERR_ALIGN, dict(Bs=ODD)), (B.DQ_ERR_ALIGN, dict(ldas=20)),
                           (B.DQ_ERR_ALIGN, dict(ldc=12)), (B.DQ_ERR_ALIGN, dict(C=ODD))]:
         assert lib.dq_gemm_mx(*changed(ok, **wrong)) == status, wrong
+    for size, most in (("M", 2 ** 26), ("N", 2 ** 26), ("K", MOST)):
+        assert lib.dq_gemm_mx(*changed(ok, **{size: most + 1})) == B.DQ_ERR_UNSUPPORTED
     assert lib.dq_gemm_mx(*changed(ok, M=0, A=None)) == B.DQ_OK and lib.dq_gemm_mx(*changed(ok, N=0)) == B.DQ_OK
 
 
