@@ -114,7 +114,7 @@ def run_config(cfg_name: str, args):
     ctx.ensure_workspace(cfg.b, cfg.n, cfg.T, xdt)
     red = B.DQ_REDUCE_TOKEN_MEAN
     objectives = {"whip": B.DQ_OBJ_WHIP, "variance": B.DQ_OBJ_VARIANCE, "kurtosis": B.DQ_OBJ_KURTOSIS,
-                  "quant": B.DQ_OBJ_QUANT}
+                  "quant": B.DQ_OBJ_QUANT, "mxfp4": B.DQ_OBJ_MXFP4, "mxfp8": B.DQ_OBJ_MXFP8}
     ctx.dq_set_objective(objectives[args.objective], 4)
 
     if args.optimizer == "cayley":
@@ -346,9 +346,9 @@ def main():
                     help="update rule: Alg. 1's SGD on the latent (the headline metric), Adam on the latent (Sec. 4.3, "
                          "Table 4), or Cayley SGD with momentum on the rotation itself (Alg. 3, the optimiser QR-Orth is "
                          "compared with in Table 4)")
-    ap.add_argument("--objective", choices=["whip", "variance", "kurtosis", "quant"], default="whip",
-                    help="what S4 evaluates: Eq. 4 (the headline metric) or one of the objectives the paper compares "
-                         "it with (Sec. 5, objective ablation)")
+    ap.add_argument("--objective", choices=["whip", "variance", "kurtosis", "quant", "mxfp4", "mxfp8"], default="whip",
+                    help="what S4 evaluates: Eq. 4 (the headline metric), one of the objectives the paper compares "
+                         "it with (Sec. 5, objective ablation) or the squared error of an MX quantiser")
     ap.add_argument("--host-batches", type=int, default=0,
                     help="also time the mini-batch loop with this many batches in pinned HOST memory "
                          "(dq_calib_run_host_batches: copies overlap the steps); reported beside the headline value, "
