@@ -511,18 +511,19 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
         }
     }
 
-    // register 4 x + y of a lane holds C[m = r][n = 8 x + 4 q + y]; lanes of the two halves exchange groups of four, so that each writes eight
-    // columns in a row: lower half 16 x .., upper half 16 x + 8 ..
+    // Register 4 x + y of a lane holds C[m = r][n = 8 x + 4 q + y]; lanes of the two halves exchange groups of four, so that each has eight columns
+    // in a row: lower half 16 x .., upper half 16 x + 8 ..  They pass through LDS, 32 rows of a wavefront at a time, and leave as whole rows of its tile.
     OUT* C = static_cast<OUT*>(g.C);
+    constexpr int CR = 32 * NI * (int)sizeof(OUT), CC = CR / 16, E = 16 / (int)sizeof(OUT), SLABS = 2 * WAVES * 32 * CR <= S::kLds ? 2 : 1;
+    static_assert(SLABS * WAVES * 32 * CR <= S::kLds, "32 rows of every wavefront have to fit");
+    const auto chunk_at = [](int row, int c) { return row * CR + 16 * (c ^ swizzle<(CC < 8 ? 4 : 8)>(row)); };
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        const int m = m0 + wm + 32 * i + r;
-        OUT* row = C + (long)m * g.ldc;
+        unsigned char* const slab = smem + (wave * SLABS + i % SLABS) * 32 * CR;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int n = n0 + wn + 32 * j + 16 * x + 8 * q;
                 unsigned w[8];
                 constexpr int W = sizeof(OUT) == 4 ? 4 : 2;       // words of four values
                 if constexpr (sizeof(OUT) == 4) {
@@ -541,20 +542,32 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
                     w[v] = e[0];
                     w[v + W] = e[1];
                 }
-                if (m >= g.M || n >= g.N) continue;
-                if (n + 8 <= g.N) {
-                    *reinterpret_cast<uint4*>(row + n) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<uint4*>(row + n + 4) = make_uint4(w[4], w[5], w[6], w[7]);
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 7; ++v)
-                        if (n + v < g.N) {
-                            if constexpr (sizeof(OUT) == 4) row[n + v] = __uint_as_float(w[v]);
-                            else row[n + v] = (bf16_t)(v & 1 ? w[v / 2] >> 16 : w[v / 2] & 0xffffu);
-                        }
-                }
+                const int c = (32 * j + 16 * x + 8 * q) / E;
+                *reinterpret_cast<uint4*>(slab + chunk_at(r, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                if constexpr (sizeof(OUT) == 4) *reinterpret_cast<uint4*>(slab + chunk_at(r, c + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
             }
         }
+        asm volatile("" ::: "memory");       // what follows reads what other lanes of the wavefront wrote
+#pragma unroll
+        for (int p = 0; p < CC / 2; ++p) {
+            const int row = (64 * p + lane) / CC, c = (64 * p + lane) % CC;
+            const uint4 w = *reinterpret_cast<const uint4*>(slab + chunk_at(row, c));
+            const int m = m0 + wm + 32 * i + row, n = n0 + wn + E * c;
+            OUT* const to = C + (long)m * g.ldc + n;
+            if (m >= g.M || n >= g.N) continue;
+            if (n + E <= g.N) {
+                *reinterpret_cast<uint4*>(to) = w;
+            } else {
+                const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int v = 0; v < E - 1; ++v)
+                    if (n + v < g.N) {
+                        if constexpr (sizeof(OUT) == 4) to[v] = __uint_as_float(u[v]);
+                        else to[v] = (bf16_t)(v & 1 ? u[v / 2] >> 16 : u[v / 2] & 0xffffu);
+                    }
+            }
+        }
+        asm volatile("" ::: "memory");
     }
 }
 
