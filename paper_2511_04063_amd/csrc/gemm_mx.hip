@@ -57,7 +57,7 @@ __device__ __forceinline__ Codes<F> load_codes(const unsigned char* row, int ste
     return c;
 }
 
-// codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale, in bf16
+// codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale, in bf16; scale 255 makes the conversions' results NaN
 template <int F, int J>
 __device__ __forceinline__ bf16x8 values8(const Codes<F>& c, unsigned byte) {
     const float s = mx_scale(byte);
@@ -77,7 +77,7 @@ __device__ __forceinline__ bf16x8 values8(const Codes<F>& c, unsigned byte) {
     }
     i32x4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = byte == 255u ? 0x7fc07fc0 : (int)w[i];
+    for (int i = 0; i < 4; ++i) r[i] = (int)w[i];
     return __builtin_bit_cast(bf16x8, r);
 }
 

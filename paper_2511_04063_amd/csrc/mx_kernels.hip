@@ -163,8 +163,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const unsigned char*
     if (left <= 0) return;
     for (long r = row; r < T; r += step) {
         const unsigned char* src = codes + r * ldc;
-        const unsigned byte = scales[r * lds + unit / LANES];
-        const float s = mx_scale(byte);
+        const float s = mx_scale(scales[r * lds + unit / LANES]);      // of 255 an infinity, which makes the conversions' results NaN
         float v[V];
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) {
@@ -177,7 +176,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const unsigned char*
                 mx_decode4<F, 0>(reinterpret_cast<const unsigned*>(src)[unit * (V / 4) + q], s, t);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * q + i] = byte == 255u ? __uint_as_float(0x7fc00000u) : t[i];
+            for (int i = 0; i < 4; ++i) v[4 * q + i] = t[i];
         }
         store_piece(Y + r * ldy + (long)unit * V, left, v);
     }
@@ -346,7 +345,7 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
                 float ss = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    e[i] = byte == 255u ? __uint_as_float(0x7fc00000u) : v[i] - e[i];
+                    e[i] = v[i] - e[i];          // NaN in a block of scale 255
                     ss += e[i] * e[i];
                     e[i] *= f;
                 }
