@@ -405,6 +405,8 @@ hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
     }
     return hipSuccess;
 }
+// Threads and pieces by a row's length: a wavefront a row where that is enough, else a workgroup; pieces that a row does not have cost loads of what
+// is there already and registers (1023 x 5004 fp32: 8 pieces 14.7 us, 5 pieces 13.4).
 template <class IN, int F>
 hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
     if constexpr (Piece<IN>::V == 8) {
@@ -412,12 +414,15 @@ hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
         if (m.n <= 1024) return norm_launch<IN, F, 2, 64>(m, s);
         if (m.n <= 2048) return norm_launch<IN, F, 1, 256>(m, s);
         if (m.n <= 4096) return norm_launch<IN, F, 2, 256>(m, s);
+        if (m.n <= 6144) return norm_launch<IN, F, 3, 256>(m, s);
         if (m.n <= 8192) return norm_launch<IN, F, 4, 256>(m, s);
     } else {
         if (m.n <= 512) return norm_launch<IN, F, 2, 64>(m, s);
         if (m.n <= 1024) return norm_launch<IN, F, 4, 64>(m, s);
         if (m.n <= 2048) return norm_launch<IN, F, 2, 256>(m, s);
         if (m.n <= 4096) return norm_launch<IN, F, 4, 256>(m, s);
+        if (m.n <= 5120) return norm_launch<IN, F, 5, 256>(m, s);
+        if (m.n <= 6144) return norm_launch<IN, F, 6, 256>(m, s);
         if (m.n <= 8192) return norm_launch<IN, F, 8, 256>(m, s);
     }
     return hipErrorInvalidValue;
