@@ -107,8 +107,10 @@ __device__ __forceinline__ void store4(OUT* dst, int left, f32x4 v) {
     }
 }
 
-// ---- straight from memory, for a few rows: a workgroup of 8 wavefronts makes 16 rows x 16 NT columns of C.  Each wavefront takes every eighth piece of 512 of the
-// reduction (a row's 16 scales, one load) and has all of a piece's operands under way at once; the eight sums are added in order through LDS.
+// ---- straight from memory, for a few rows: a workgroup of 8 wavefronts makes 16 rows x 16 NT columns of C.  Each wavefront takes every eighth piece
+// of 512 of the reduction (a row's 16 scales, one load) and has all of a piece's operands under way at once; the eight sums are added in order
+// through LDS.  Bound by one latency from launch to store: 1 x 4096, 4096 of 4 x 4 bits 4.0 us, of which a kernel of no work takes 2 and the 8.9 MB
+// of B, at the rate of a large copy, 1.7.
 template <int FA, int FB, class OUT, int NT>
 __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles_n) {
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
@@ -192,6 +194,11 @@ hipError_t launch_direct(const GemmMx& g, hipStream_t s) {
 // kStages - 2 later stages still travelling, then a barrier; behind it stage i + 1 is complete in LDS, and every wavefront has read the last of stage i,
 // whose place the parts of stage i + kStages take.
 // The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for 512 of the reduction, the same way.
+//
+// What bounds it.  256 x 256 tiles: the matrix cores and their power.  8192^3 of 4 x 4 bits takes 288 us (3.8 PFLOP/s), of 8 x 8 407 (2.7; the
+// library's product of plain fp8 matrices 398): the matrix cores are busy 57 and 70 % of the cycles, and the clock falls from 2.4 to 1.73 and 1.85 GHz.
+// A step of 64 costs 550 cycles of 512 in the matrix cores, and a round of tiles 12 us around its steps: 33 MB of C, the first loads, the launch.
+// fp32 results of 8-bit operands: bf16 arithmetic, 8192^3 890 us (1.24 PFLOP/s; the library's bf16 product 1.30).  Few tiles: latency of the loads.
 //
 // LDS holds rows of 64 or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
 // different banks, and so do sixteen (no conflicts are counted).
@@ -580,15 +587,16 @@ hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Which kernel, by what each takes for C = M x N, K (us of the kernel alone; 4 x 4 bits unless said):
+// Which kernel, by what each takes for C = M x N, K (us of the kernel alone, operands in the caches; 4 x 4 bits and bf16 unless said):
 //   straight from memory against 64 x 32 tiles      1 x 4096, 4096: 3.9, 6.1;  16 x 4096, 4096 (8 x 8): 6.8, 7.8;  but 16 x 8192, 8192 (8 x 8): 20.0, 13.3;
 //                                                   24 x 8192, 4096 (8 x 4; 32 rows of the first kernel): 7.5, 6.7
-//   64 x 32 tiles, 4 groups against 64 x 64, 2      128 x 4096, 4096: 5.7, 6.6;  256 x 4096, 4096 (512 and 256 workgroups): 11.1, 7.2
-//   64 x 64 tiles against 128 x 64, 2 groups        256 x 4096, 4096: 7.2, 8.7;  512 x 4096, 4096 (512 and 256 workgroups): 11.4, 9.8
-//   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 9.8, 11.4;  1024 x 4096, 4096: 18.7, 14.7
-//   128 x 128 tiles, four stages in LDS against two   operands not in the L2s: 1024 x 4096, 4096 (256 workgroups): 17.1, 22.1;  2048 x 4096, 4096 (512): 32.5, 29.3
-//   128 x 128 tiles against 256 x 256               2048 x 4096, 4096 (512 and 128 workgroups): 25.4, 26.5
-// that is, the largest tile that still gives most compute units a workgroup.  A kernel of no work takes 2 us, one of 64 in the reduction 4 to 5.
+//   64 x 32 tiles, 4 groups against 64 x 64, 2      128 x 4096, 4096: 6.8, 7.4;  256 x 4096, 4096 (512 and 256 workgroups): 12.2, 8.4
+//   64 x 64 tiles against 128 x 64, 2 groups        256 x 4096, 4096: 8.4, 9.9;  512 x 4096, 4096 (512 and 256 workgroups): 12.1, 10.8
+//   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 10.8, 12.3;  1024 x 4096, 4096: 19.3, 14.4
+//   128 x 128 tiles, all of LDS against half          operands not in the L2s: 1024 x 4096, 4096 (256 workgroups): 17.1, 22.1;  2048 x 4096, 4096 (512): 32.5, 29.3
+//   128 x 128 tiles against 256 x 256               2048 x 4096, 4096 (512 and 128 workgroups): 25.0, 29.0
+// that is, the largest tile that still gives most compute units a workgroup.  (256 x 128 tiles in between: 24.3 for the last, but 39.7 against 37.6 for
+// 2560 x 4096, and 46.6 against 40.8 for 4096 x 4096, 1024 in bf16 arithmetic.)  A kernel of no work takes 2 us, one of 64 in the reduction 4 to 5.
 template <int FA, int FB, class OUT>
 hipError_t launch_types(const GemmMx& g, hipStream_t s) {
     constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
@@ -600,8 +608,8 @@ hipError_t launch_types(const GemmMx& g, hipStream_t s) {
     const auto tiles = [&](long tm, long tn) { return ((g.M + tm - 1) / tm) * ((g.N + tn - 1) / tn); };
     constexpr long most = 192;
     if (!exact && tiles(256, 256) >= most) {
-        // eight wavefronts to a tile for 4 x 4 bits (8192^3: 324 -> 299 us), four for the others, whose fragments do not leave registers for two
-        // wavefronts a SIMD (8 x 8 bits: 429 us against 476)
+        // Eight wavefronts to a tile for 4 x 4 bits (8192^3: 324 us with four, 299), four for the others, whose fragments do not leave registers for two
+        // wavefronts a SIMD (8 x 8 bits: 429 us, 476 with eight).
         if constexpr (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8, 1, 160>(g, s);
         else if constexpr (!exact) return launch_tile<FA, FB, OUT, 4, 4, 4, 1, 160>(g, s);
     }
