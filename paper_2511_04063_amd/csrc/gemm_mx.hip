@@ -520,13 +520,12 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
 
     // Register 4 x + y of a lane holds C[m = r][n = 8 x + 4 q + y]; lanes of the two halves exchange groups of four, so that each has eight columns
     // in a row: lower half 16 x .., upper half 16 x + 8 ..  They pass through LDS, 32 rows of a wavefront at a time, and leave as whole rows of its tile.
-    OUT* C = static_cast<OUT*>(g.C);
-    constexpr int CR = 32 * NI * (int)sizeof(OUT), CC = CR / 16, E = 16 / (int)sizeof(OUT), SLABS = 2 * WAVES * 32 * CR <= S::kLds ? 2 : 1;
-    static_assert(SLABS * WAVES * 32 * CR <= S::kLds, "32 rows of every wavefront have to fit");
+    // While 32 rows are on their way back from LDS the next 32 are written to it.
+    constexpr int CR = 32 * NI * (int)sizeof(OUT), CC = CR / 16, E = 16 / (int)sizeof(OUT);
+    static_assert(2 * WAVES * 32 * CR <= S::kLds, "twice 32 rows of every wavefront have to fit");
     const auto chunk_at = [](int row, int c) { return row * CR + 16 * (c ^ swizzle<(CC < 8 ? 4 : 8)>(row)); };
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        unsigned char* const slab = smem + (wave * SLABS + i % SLABS) * 32 * CR;
+    const auto put_rows = [&](int i) {
+        unsigned char* const slab = smem + (2 * wave + (i & 1)) * 32 * CR;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
 #pragma unroll
@@ -554,26 +553,43 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
                 if constexpr (sizeof(OUT) == 4) *reinterpret_cast<uint4*>(slab + chunk_at(r, c + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
             }
         }
-        asm volatile("" ::: "memory");       // what follows reads what other lanes of the wavefront wrote
+    };
+    OUT* const C = static_cast<OUT*>(g.C);
+    const bool inside = m0 + S::TM <= g.M && n0 + S::TN <= g.N;
+    const auto send_rows = [&](int i) {
+        const unsigned char* const slab = smem + (2 * wave + (i & 1)) * 32 * CR;
+        uint4 w[CC / 2];
+#pragma unroll
+        for (int p = 0; p < CC / 2; ++p) w[p] = *reinterpret_cast<const uint4*>(slab + chunk_at((64 * p + lane) / CC, (64 * p + lane) % CC));
+        const int m = m0 + wm + 32 * i + lane / CC, n = n0 + wn + E * (lane % CC);
+        OUT* const to = C + (long)m * g.ldc + n;
+        if (inside) {
+#pragma unroll
+            for (int p = 0; p < CC / 2; ++p) *reinterpret_cast<uint4*>(to + (long)(64 / CC * p) * g.ldc) = w[p];
+            return;
+        }
 #pragma unroll
         for (int p = 0; p < CC / 2; ++p) {
-            const int row = (64 * p + lane) / CC, c = (64 * p + lane) % CC;
-            const uint4 w = *reinterpret_cast<const uint4*>(slab + chunk_at(row, c));
-            const int m = m0 + wm + 32 * i + row, n = n0 + wn + E * c;
-            OUT* const to = C + (long)m * g.ldc + n;
-            if (m >= g.M || n >= g.N) continue;
+            if (m + 64 / CC * p >= g.M || n >= g.N) continue;
+            OUT* const at = to + (long)(64 / CC * p) * g.ldc;
             if (n + E <= g.N) {
-                *reinterpret_cast<uint4*>(to) = w;
+                *reinterpret_cast<uint4*>(at) = w[p];
             } else {
-                const unsigned u[4] = {w.x, w.y, w.z, w.w};
+                const unsigned u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
 #pragma unroll
                 for (int v = 0; v < E - 1; ++v)
                     if (n + v < g.N) {
-                        if constexpr (sizeof(OUT) == 4) to[v] = __uint_as_float(u[v]);
-                        else to[v] = (bf16_t)(v & 1 ? u[v / 2] >> 16 : u[v / 2] & 0xffffu);
+                        if constexpr (sizeof(OUT) == 4) at[v] = __uint_as_float(u[v]);
+                        else at[v] = (bf16_t)(v & 1 ? u[v / 2] >> 16 : u[v / 2] & 0xffffu);
                     }
             }
         }
+    };
+#pragma unroll
+    for (int i = 0; i <= MI; ++i) {
+        if (i < MI) put_rows(i < MI ? i : 0);
+        asm volatile("" ::: "memory");       // lanes read what other lanes of their wavefront wrote
+        if (i > 0) send_rows(i - 1);
         asm volatile("" ::: "memory");
     }
 }
