@@ -107,78 +107,92 @@ __device__ __forceinline__ void store4(OUT* dst, int left, f32x4 v) {
     }
 }
 
-// ---- straight from memory, for a few rows: a workgroup of 8 wavefronts makes 16 rows x 16 NT columns of C.  Each wavefront takes every eighth piece
-// of 512 of the reduction (a row's 16 scales, one load) and has all of a piece's operands under way at once; the eight sums are added in order
-// through LDS.  Bound by one latency from launch to store: 1 x 4096, 4096 of 4 x 4 bits 4.0 us, of which a kernel of no work takes 2 and the 8.9 MB
-// of B, at the rate of a large copy, 1.7.
-template <int FA, int FB, class OUT, int NT>
+// ---- straight from memory, for small products: a workgroup of 8 wavefronts makes 16 MT rows x 16 NT columns of C.  Each wavefront takes every
+// eighth piece of 512 of the reduction (a row's 16 scales, one load) and has all of a piece's operands under way at once; the eight sums are added in
+// order through LDS.  Bound by one latency from launch to store: 1 x 4096, 4096 of 4 x 4 bits 4.0 us, of which a kernel of no work takes 2 and the 8.9
+// MB of B, at the rate of a large copy, 1.7; 300 x 300, 300 3.0.
+template <int FA, int FB, class OUT, int MT, int NT>
 __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles_n) {
     constexpr bool EXACT = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
-    __shared__ f32x4 part[8][NT][64];
+    __shared__ f32x4 part[8][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * (16 * NT), m0 = (int)(blockIdx.x / (unsigned)tiles_n) * 16;
+    const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * (16 * NT), m0 = (int)(blockIdx.x / (unsigned)tiles_n) * (16 * MT);
     const int nb = (int)((g.K + 31L) / 32);
-    const int row_a = m0 + r < g.M ? m0 + r : g.M - 1;
-    const unsigned char *pa = g.A + (long)row_a * g.lda, *sa = g.As + (long)row_a * g.ldas, *pb[NT], *sb[NT];
+    const unsigned char *pa[MT], *sa[MT], *pb[NT], *sb[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int row = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
+        pa[i] = g.A + (long)row * g.lda;
+        sa[i] = g.As + (long)row * g.ldas;
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int row = n0 + 16 * j + r < g.N ? n0 + 16 * j + r : g.N - 1;
         pb[j] = g.B + (long)row * g.ldb;
         sb[j] = g.Bs + (long)row * g.ldbs;
     }
-    f32x4 acc[NT];
+    f32x4 acc[MT][NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int piece = wave; 16 * piece < nb; piece += 8) {
-        Codes<FA> a[4];
+        Codes<FA> a[4][MT];
         Codes<FB> b[4][NT];
-        i32x4 ea, eb[NT];
+        i32x4 ea[MT], eb[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) eb[j] = *reinterpret_cast<const i32x4*>(sb[j] + 16L * piece);
-        ea = *reinterpret_cast<const i32x4*>(sa + 16L * piece);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) ea[i] = *reinterpret_cast<const i32x4*>(sa[i] + 16L * piece);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) b[t][j] = load_codes<FB, EXACT>(pb[j], 4 * piece + t, q, nb);
-            a[t] = load_codes<FA, EXACT>(pa, 4 * piece + t, q, nb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[t][i] = load_codes<FA, EXACT>(pa[i], 4 * piece + t, q, nb);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const bool in = 16 * piece + 4 * t + q < nb;          // what lies behind a row's last scale may be anything
-            const unsigned xa = in ? (unsigned)ea[t] >> (8 * q) : 0u;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const unsigned xb = in ? (unsigned)eb[j][t] >> (8 * q) : 0u;
-                if constexpr (EXACT) acc[j] = mfma_values<FB, FA>(b[t][j], a[t], acc[j], xb & 255u, xa & 255u);
-                else acc[j] = mfma_mx<FB, FA>(b[t][j], a[t], acc[j], (int)xb, (int)xa);
+            for (int i = 0; i < MT; ++i) {
+                const unsigned xa = in ? (unsigned)ea[i][t] >> (8 * q) : 0u;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const unsigned xb = in ? (unsigned)eb[j][t] >> (8 * q) : 0u;
+                    if constexpr (EXACT) acc[i][j] = mfma_values<FB, FA>(b[t][j], a[t][i], acc[i][j], xb & 255u, xa & 255u);
+                    else acc[i][j] = mfma_mx<FB, FA>(b[t][j], a[t][i], acc[i][j], (int)xb, (int)xa);
+                }
             }
         }
     }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) part[wave][j][lane] = acc[j];
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[wave][i * NT + j][lane] = acc[i][j];
     __syncthreads();
-    if (wave < NT) {
+    if (wave < MT * NT) {
         f32x4 c = part[0][wave][lane];
 #pragma unroll
         for (int k = 1; k < 8; ++k) c += part[k][wave][lane];
-        const int m = m0 + r, n = n0 + 16 * wave + 4 * q;
+        const int m = m0 + wave / NT * 16 + r, n = n0 + wave % NT * 16 + 4 * q;
         if (m < g.M && n < g.N) store4(static_cast<OUT*>(g.C) + (long)m * g.ldc + n, g.N - n, c);
     }
 }
 
-template <int FA, int FB, class OUT, int NT>
+template <int FA, int FB, class OUT, int MT, int NT>
 hipError_t launch_direct(const GemmMx& g, hipStream_t s) {
-    const long tn = (g.N + 16L * NT - 1) / (16 * NT), tm = (g.M + 15L) / 16;
+    const long tn = (g.N + 16L * NT - 1) / (16 * NT), tm = (g.M + 16L * MT - 1) / (16 * MT);
     // a launch counts its threads in 32 bits: 2^31 of them at a time
     const long band = tn < (1L << 22) ? (1L << 22) / tn : 1;
     for (long first = 0; first < tm; first += band) {
-        const long strips = tm - first < band ? tm - first : band, row = 16 * first;
+        const long strips = tm - first < band ? tm - first : band, row = 16 * MT * first;
         GemmMx p = g;
         p.A = g.A + row * g.lda;
         p.As = g.As + row * g.ldas;
         p.C = static_cast<OUT*>(g.C) + row * g.ldc;
-        p.M = (int)(g.M - row < 16 * strips ? g.M - row : 16 * strips);
-        hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, NT>), dim3((unsigned)(strips * tn)), dim3(512), 0, s, p, (int)tn);
+        p.M = (int)(g.M - row < 16 * MT * strips ? g.M - row : 16 * MT * strips);
+        hipLaunchKernelGGL((gemm_mx_direct_kernel<FA, FB, OUT, MT, NT>), dim3((unsigned)(strips * tn)), dim3(512), 0, s, p, (int)tn);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -604,8 +618,12 @@ hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
 }
 
 // Which kernel, by what each takes for C = M x N, K (us of the kernel alone, operands in the caches; 4 x 4 bits and bf16 unless said):
-//   straight from memory against 64 x 32 tiles      1 x 4096, 4096: 3.9, 6.1;  16 x 4096, 4096 (8 x 8): 6.8, 7.8;  but 16 x 8192, 8192 (8 x 8): 20.0, 13.3;
-//                                                   24 x 8192, 4096 (8 x 4; 32 rows of the first kernel): 7.5, 6.7
+//   straight from memory, 16 rows, against 64 x 32 tiles   1 x 4096, 4096: 4.0, 6.1;  1 x 4096, 16384: 8.2, 11.8;  16 x 4096, 8192 (8 x 8): 11.1, 12.3;
+//                                                   16 x 8192, 4096: 6.0, 6.3;  but 16 x 8192, 8192: 9.8, 8.8, and 1 x 8192, 8192 (8 x 8, fp32) 20.3, 16.4
+//   the same, 32 rows x 16 (256 workgroups at most)   17 x 1000, 2000 (8 x 4): 3.8, 5.7;  300 x 300, 300 (8 x 8, fp32): 3.9, 7.3;  24 x 4096, 4096 (8 x 4): 7.2,
+//                                                   7.4;  but 24 x 8192, 2048 (512): 7.9, 6.1, and 64 x 1000, 8192 (8 x 4): 12.5, 9.8
+//   the same, 32 rows x 32 (256 workgroups at most)   24 x 8192, 2048 (8 x 4): 5.5, 6.1;  512 x 512, 512 (8 x 8, fp32): 5.0, 7.4;  but 24 x 8192, 4096 (8 x
+//                                                   4): 8.7, 8.1, and 1000 x 1000, 256 (1024): 8.4, 5.6
 //   64 x 32 tiles, 4 groups against 64 x 64, 2      128 x 4096, 4096: 6.8, 7.4;  256 x 4096, 4096 (512 and 256 workgroups): 12.2, 8.4
 //   64 x 64 tiles against 128 x 64, 2 groups        256 x 4096, 4096: 8.4, 9.9;  512 x 4096, 4096 (512 and 256 workgroups): 12.1, 10.8
 //   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 10.8, 12.3;  1024 x 4096, 4096: 19.3, 14.4
@@ -617,11 +635,13 @@ template <int FA, int FB, class OUT>
 hipError_t launch_types(const GemmMx& g, hipStream_t s) {
     constexpr bool exact = sizeof(OUT) == 4 && (FA == DQ_MXFP8 || FB == DQ_MXFP8);
     const bool near_rows = g.lda < (1L << 23) && g.ldb < (1L << 23);       // the tiles address their rows by 32-bit offsets
-    if (!near_rows || (g.M <= 16 && g.K <= 4096)) {
-        // 32 columns a workgroup as soon as that gives every compute unit one: 1 x 8192, 8192 8.1 -> 7.7 us
-        return g.N >= 32 * 256 ? launch_direct<FA, FB, OUT, 2>(g, s) : launch_direct<FA, FB, OUT, 1>(g, s);
-    }
     const auto tiles = [&](long tm, long tn) { return ((g.M + tm - 1) / tm) * ((g.N + tn - 1) / tn); };
+    if (!near_rows || (g.M <= 16 && (g.K <= 4096 || tiles(16, 16) <= 256))) {
+        // 32 columns a workgroup as soon as that gives every compute unit one: 1 x 8192, K 8192 8.1 -> 7.7 us
+        return g.N >= 32 * 256 ? launch_direct<FA, FB, OUT, 1, 2>(g, s) : launch_direct<FA, FB, OUT, 1, 1>(g, s);
+    }
+    if (g.K <= 4096 && tiles(32, 16) <= 256) return launch_direct<FA, FB, OUT, 2, 1>(g, s);
+    if (g.K <= 2560 && tiles(32, 32) <= 256) return launch_direct<FA, FB, OUT, 2, 2>(g, s);
     constexpr long most = 192;
     if (!exact && tiles(256, 256) >= most) {
         // Eight wavefronts to a tile for 4 x 4 bits (8192^3: 324 us with four, 299), four for the others, whose fragments do not leave registers for two

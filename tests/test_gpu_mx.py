@@ -353,7 +353,7 @@ def test_gemm_mx(ctx, fa, fb, cdt, M, N, K):
 
 # Shapes that are multiples of no tile, for each kernel that the size of the result chooses (256, 128 with more and with fewer workgroups than compute
 # units, 128 x 64, 64, 64 x 32, up to 16 rows with a long reduction), with reductions of one block, of odd counts of stages and of pieces of 512
-@pytest.mark.parametrize("M,N", [(3601, 3570), (2049, 2190), (1701, 1750), (1000, 1601), (801, 1000), (200, 333), (9, 700)])
+@pytest.mark.parametrize("M,N", [(3601, 3570), (2049, 2190), (1701, 1750), (1000, 1601), (801, 1000), (400, 701), (200, 333), (100, 1503), (9, 700)])
 @pytest.mark.parametrize("K", [20, 545, 1700, 5200])
 @pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (0, 1), (1, 1)])
@@ -397,7 +397,7 @@ def test_gemm_of_rows_far_apart(ctx, fa, fb):
 
 @pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (0, 1), (1, 1)])
-@pytest.mark.parametrize("M,N,K", [(5, 40, 600), (300, 280, 600), (1000, 1601, 600), (1701, 1750, 600), (3601, 3570, 600)])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 600), (30, 41, 600), (100, 1503, 600), (300, 280, 600), (400, 701, 600), (1000, 1601, 600), (1701, 1750, 600), (3601, 3570, 600)])
 def test_gemm_of_blocks_that_are_nan(ctx, M, N, K, fa, fb, cdt):
     a, A, As = random_matrix(M, K, fa, 71)
     b, Bm, Bs = random_matrix(N, K, fb, 72)
