@@ -311,9 +311,9 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 // Squared error of the MX quantiser and its derivative:  loss_t = (1/n) sum_i (y_i - yhat_i)^2,  dY_i = c (2/n) (y_i - yhat_i).  yhat is
 // constant around almost every y (the scale is a power of two), so this is the derivative wherever there is one.
 //
-// A workgroup takes the pieces of a row group (a long row, or rg short ones side by side) 4 x 256 at a time, or those of four groups of short rows,
-// all four under way together.  Bound by HBM: 8192 x 4096 with a bf16 gradient, 201 MB, 35.3 us (5.7 TB/s); 64 problems of 2048 x 128 with an fp32
-// one, 134 MB, 26.7 us (5.0 TB/s).
+// A workgroup takes the pieces of a long row 4 x 256 at a time, or those of four groups of rows of up to 1024 values (rg side by side), all four under
+// way together (10 problems of 2849 x 648: 53 us a row at a time, 37; but two rows of up to 2048 values each: 8192 x 2048 30 -> 34).  Bound by HBM: 8192 x
+// 4096 with a bf16 gradient, 201 MB, 35.3 us (5.7 TB/s); 64 problems of 2048 x 128 with an fp32 one, 134 MB, 26.7 us (5.0 TB/s).
 template <int F, bool BF16OUT>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
                                                            long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
     __shared__ double tot[4];
     Y += (long)blockIdx.y * sy;
     const float f = scale * 2.f / (float)n;
-    const bool side = w.rg > 1;
+    const bool side = w.upr <= 256;
     const int r_in = side ? (int)threadIdx.x / w.upr : 0, u_in = side ? (int)threadIdx.x - r_in * w.upr : (int)threadIdx.x;
     const long groups = ((long)T + w.rg - 1) / w.rg;
     const long row_step = side ? (long)gridDim.x * w.rg : 0, hop = side ? U * (long)gridDim.x : gridDim.x;
@@ -470,9 +470,12 @@ hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s) {
     return m.format == DQ_MXFP4 ? norm_shape<float, DQ_MXFP4>(m, s) : norm_shape<float, DQ_MXFP8>(m, s);
 }
 
+// four row groups of short rows a workgroup; of the wider ones fewer where that would leave compute units without one (64 x 1000: 6.4 -> 5.2 us; not of
+// narrow ones, which come in batches: 64 problems of 2048 x 128 29 -> 39)
 int mx_objective_grid(int T, int n) {
     const Walk w = make_walk(n, 4);
-    const long groups = ((long)T + w.rg - 1) / w.rg, g = w.rg > 1 ? (groups + 3) / 4 : groups;
+    const long groups = ((long)T + w.rg - 1) / w.rg, few = groups < 256 ? groups : 256, fourth = (groups + 3) / 4;
+    const long g = w.upr > 256 ? groups : w.rg > 1 || fourth > few ? fourth : few;
     return (int)(g < 2048 ? g : 2048);
 }
 

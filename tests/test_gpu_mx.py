@@ -258,7 +258,7 @@ def test_objective_of_many_rows_and_of_many_problems(ctx):
             assert abs(loss[i].item() - ref_loss) <= 8 * 2.0 ** -24 * ref_loss
 
 
-@pytest.mark.parametrize("b,T,n", [(1, 1, 1), (1, 5, 33), (3, 45, 640), (1, 37, 101), (64, 9, 128), (2, 300, 80), (1, 19, 1500), (1, 9, 4096), (1, 5, 8192), (1, 7, 5001)])
+@pytest.mark.parametrize("b,T,n", [(1, 1, 1), (1, 5, 33), (3, 45, 640), (1, 37, 101), (64, 9, 128), (2, 300, 80), (1, 19, 1500), (1, 9, 4096), (1, 5, 8192), (1, 7, 5001), (1, 9001, 530)])
 @pytest.mark.parametrize("grad", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_objective(ctx, fmt, grad, b, T, n):
