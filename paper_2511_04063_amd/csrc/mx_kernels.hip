@@ -9,9 +9,9 @@ namespace {
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-template <class T> struct Piece;                       // what one 16-byte access holds
-template <> struct Piece<float> { static constexpr int V = 4; };
-template <> struct Piece<bf16_t> { static constexpr int V = 8; };
+template <class T> struct Piece;                       // what one 16-byte access holds, and the access at any element
+template <> struct Piece<float> { static constexpr int V = 4; typedef u32x4 Anywhere __attribute__((aligned(4))); };
+template <> struct Piece<bf16_t> { static constexpr int V = 8; typedef u32x4 Anywhere __attribute__((aligned(2))); };
 
 __device__ __forceinline__ unsigned bf16_pair(float a, float b) {
     const mx_f32x2 v = {a, b};
@@ -30,30 +30,38 @@ __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
         v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-// The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  Whole pieces without a
-// branch; a piece that is not whole reads the row's first one instead, and again value by value afterwards.
+// The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  Without a branch: in place of a piece
+// that is not whole the row's last V values are read, and shifted to their place afterwards (the norm of 8192 x 1100 in bf16: 20.6 us with such values
+// read one by one, 17.1); value by value only of rows shorter than a piece.
 // STREAM: past the caches, for what is read once by a kernel that writes less than it reads (quantiser 8192 x 8192 42 -> 34 us, objective 8192 x 4096
 // 39 -> 35; the norm, which writes as much, 50 -> 52).
 template <bool STREAM, class T>
 __device__ __forceinline__ uint4 load_whole(const T* row, int c, int n) {
     if (n < Piece<T>::V) return make_uint4(0u, 0u, 0u, 0u);
-    const u32x4* at = reinterpret_cast<const u32x4*>(row + (c + Piece<T>::V <= n ? c : 0));
+    const typename Piece<T>::Anywhere* at = reinterpret_cast<const typename Piece<T>::Anywhere*>(row + (c + Piece<T>::V <= n ? c : n - Piece<T>::V));
     const u32x4 q = STREAM ? __builtin_nontemporal_load(at) : *at;
     return make_uint4(q.x, q.y, q.z, q.w);
 }
 template <class T>
 __device__ __forceinline__ void finish_piece(uint4& q, const T* row, int c, int n) {
-    constexpr int V = Piece<T>::V;
-    if (c + V > n) {
-        unsigned w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < V - 1; ++i)
-            if (c + i < n) {
-                if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
-                else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
-            }
-        q = make_uint4(w[0], w[1], w[2], w[3]);
+    constexpr int V = Piece<T>::V, BITS = 128 / V;
+    if (n >= V) {
+        const int over = c + V - n, by = BITS * over;        // values behind the end
+        if (over > 0) {
+            const unsigned long long lo = (unsigned long long)q.y << 32 | q.x, hi = (unsigned long long)q.w << 32 | q.z;
+            const unsigned long long low = by < 64 ? lo >> by | hi << (64 - by) : by < 128 ? hi >> (by - 64) : 0ull, high = by < 64 ? hi >> by : 0ull;
+            q = make_uint4((unsigned)low, (unsigned)(low >> 32), (unsigned)high, (unsigned)(high >> 32));
+        }
+        return;
     }
+    unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < V - 1; ++i)
+        if (c + i < n) {
+            if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
+            else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+        }
+    q = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void store_piece(float* dst, int left, const float (&v)[4]) {
     if (left >= 4) {
@@ -412,27 +420,29 @@ hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
     }
     return hipSuccess;
 }
-// Threads and pieces by a row's length: a wavefront a row where that is enough, else a workgroup; pieces that a row does not have cost loads of what
-// is there already and registers (1023 x 5004 fp32: 8 pieces 14.7 us, 5 pieces 13.4).
-template <class IN, int F>
-hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
-    if constexpr (Piece<IN>::V == 8) {
-        if (m.n <= 512) return norm_launch<IN, F, 1, 64>(m, s);
-        if (m.n <= 1024) return norm_launch<IN, F, 2, 64>(m, s);
-        if (m.n <= 2048) return norm_launch<IN, F, 1, 256>(m, s);
-        if (m.n <= 4096) return norm_launch<IN, F, 2, 256>(m, s);
-        if (m.n <= 6144) return norm_launch<IN, F, 3, 256>(m, s);
-        if (m.n <= 8192) return norm_launch<IN, F, 4, 256>(m, s);
-    } else {
-        if (m.n <= 512) return norm_launch<IN, F, 2, 64>(m, s);
-        if (m.n <= 1024) return norm_launch<IN, F, 4, 64>(m, s);
-        if (m.n <= 2048) return norm_launch<IN, F, 2, 256>(m, s);
-        if (m.n <= 4096) return norm_launch<IN, F, 4, 256>(m, s);
-        if (m.n <= 5120) return norm_launch<IN, F, 5, 256>(m, s);
-        if (m.n <= 6144) return norm_launch<IN, F, 6, 256>(m, s);
-        if (m.n <= 8192) return norm_launch<IN, F, 8, 256>(m, s);
+// Pieces of a thread: as many as a row has, since others cost loads of what is there already and registers (1023 x 5004 fp32: 8 pieces 14.7 us, 5
+// pieces 13.4).
+template <class IN, int F, int TPR>
+hipError_t norm_pieces(const MxNorm& m, hipStream_t s) {
+    constexpr int V = Piece<IN>::V;
+    switch ((m.n + TPR * V - 1) / (TPR * V)) {
+        case 1: return norm_launch<IN, F, 1, TPR>(m, s);
+        case 2: return norm_launch<IN, F, 2, TPR>(m, s);
+        case 3: return norm_launch<IN, F, 3, TPR>(m, s);
+        case 4: return norm_launch<IN, F, 4, TPR>(m, s);
+        case 5: if constexpr (V == 4) return norm_launch<IN, F, 5, TPR>(m, s); break;
+        case 6: if constexpr (V == 4 && TPR == 256) return norm_launch<IN, F, 6, TPR>(m, s); break;
+        case 7: if constexpr (V == 4 && TPR == 256) return norm_launch<IN, F, 7, TPR>(m, s); break;
+        case 8: if constexpr (V == 4 && TPR == 256) return norm_launch<IN, F, 8, TPR>(m, s); break;
     }
     return hipErrorInvalidValue;
+}
+// A wavefront a row where 4 pieces a lane in bf16, 5 in fp32, are enough (8192 rows: 1100 in bf16 24.4 us a workgroup a row, 17.1; 1500 26.4, 20.3; 1030
+// in fp32 26.0, 24.1; but 1500 in fp32 29.3, 30.4), unless there are few rows (400 x 1000 fp32: 4.4, 3.4 a workgroup a row; 600 x 1500 bf16 5.2, 4.5).
+template <class IN, int F>
+hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
+    constexpr int V = Piece<IN>::V;
+    return m.n <= 64 * V || (m.n <= 64 * V * (V == 8 ? 4 : 5) && m.T > 1024) ? norm_pieces<IN, F, 64>(m, s) : norm_pieces<IN, F, 256>(m, s);
 }
 
 }  // namespace

@@ -162,7 +162,8 @@ def test_large_inputs_give_the_codes_of_their_parts(ctx, fmt, xdt):
 
 
 # ----------------------------------------------------------------------------------- norm
-NORM_SHAPES = [(1, 1), (3, 33), (130, 40), (5, 300), (4, 512), (9, 513), (6, 1000), (3, 1024), (5, 2048), (2, 2890), (1, 4096), (7, 4100), (9, 5004), (2, 5120), (5, 5800), (4, 6145), (3, 8192), (0, 64)]
+NORM_SHAPES = [(1, 1), (3, 33), (130, 40), (5, 300), (4, 512), (9, 513), (6, 1000), (3, 1024), (5, 2048), (2, 2890), (1, 4096), (7, 4100), (9, 5004), (2, 5120), (5, 5800), (4, 6145), (3, 8192), (0, 64),
+               (1030, 700), (1025, 1101), (1029, 1279), (1026, 2046), (1500, 129)]
 
 
 def norm_reference(X, res, dtype, gain, eps, fmt):
