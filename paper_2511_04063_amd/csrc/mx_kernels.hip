@@ -122,42 +122,42 @@ __device__ __forceinline__ void put_blocks(const float (&v)[NV], int unit, int n
     }
 }
 
-// Threads over rows of `upr` pieces: `rg` whole rows side by side in a workgroup where they are short (rg * upr <= 256), else tiles of 256
-// pieces along a row (blockIdx.x); rows are walked in steps of rg * gridDim.y, so that a thread stays at its column.
-struct Walk { int upr, rg; };
-__device__ __forceinline__ bool walk_start(const Walk& w, int& row, int& unit) {
-    if (w.rg > 1) {
-        const int r = (int)threadIdx.x / w.upr;
-        unit = (int)threadIdx.x - r * w.upr;
-        row = (int)blockIdx.y * w.rg + r;
-        return r < w.rg;
-    }
-    unit = (int)(blockIdx.x * 256 + threadIdx.x);
-    row = (int)blockIdx.y;
-    return unit < w.upr;
+// Threads over all pieces of all rows, `upr` a row: a thread's next piece is 256 times the grid further on, `rows` rows and `units` pieces.
+struct Walk { int upr; unsigned rows; int units; };
+struct Place { unsigned row; int unit; };
+__device__ __forceinline__ Place walk_start(const Walk& w) {
+    const unsigned item = blockIdx.x * 256 + threadIdx.x, row = item / (unsigned)w.upr;
+    return Place{row, (int)(item - row * (unsigned)w.upr)};
+}
+__device__ __forceinline__ Place walk_next(const Walk& w, const Place& at) {
+    const int unit = at.unit + w.units;
+    return unit < w.upr ? Place{at.row + w.rows, unit} : Place{at.row + w.rows + 1, unit - w.upr};
 }
 
-// Bound by HBM; U rows of a thread under way at a time, or a row's latency shows (8192 x 8192 bf16 to 4 bits, 170 MB, 42 -> 34 us with the loads past
+// Bound by HBM; U pieces of a thread under way at a time, or their latency shows (8192 x 8192 bf16 to 4 bits, 170 MB, 42 -> 34 us with the loads past
 // the caches: 5.0 TB/s, a large copy reaches 5.3; 333 x 2890, 5 MB: 3.7 us, 2 of them a kernel's own).
 template <class IN, int F>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__ X, long ldx, int T, int n, int nb, unsigned char* __restrict__ codes,
                                                           long ldc, unsigned char* __restrict__ scales, long lds, Walk w, unsigned* flags) {
     constexpr int V = Piece<IN>::V, U = 4;
-    int row, unit;
-    if (!walk_start(w, row, unit)) return;
-    const long step = (long)w.rg * gridDim.y;
-    for (long r = row; r < T; r += U * step) {
+    Place at = walk_start(w);
+    while (at.row < (unsigned)T) {
         uint4 q[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) q[k] = load_whole<true>(X + (r + k * step < T ? r + k * step : r) * ldx, unit * V, n);
+        Place p[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const long at = r + k * step;
-            if (at >= T) break;
-            finish_piece(q[k], X + at * ldx, unit * V, n);
+            p[k] = at;
+            const bool in = at.row < (unsigned)T;
+            q[k] = load_whole<true>(X + (long)(in ? at.row : 0u) * ldx, in ? at.unit * V : 0, n);
+            at = walk_next(w, at);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (p[k].row >= (unsigned)T) break;
+            finish_piece(q[k], X + (long)p[k].row * ldx, p[k].unit * V, n);
             float v[V];
             unpack(q[k], v);
-            put_blocks<F, V>(v, unit, nb, codes + at * ldc, scales + at * lds, flags);
+            put_blocks<F, V>(v, p[k].unit, nb, codes + (long)p[k].row * ldc, scales + (long)p[k].row * lds, flags);
         }
     }
 }
@@ -168,28 +168,26 @@ template <class OUT, int F>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const unsigned char* __restrict__ codes, long ldc, const unsigned char* __restrict__ scales,
                                                             long lds, int T, int n, OUT* __restrict__ Y, long ldy, Walk w) {
     constexpr int V = Piece<OUT>::V, LANES = 32 / V;
-    int row, unit;
-    if (!walk_start(w, row, unit)) return;
-    const int step = w.rg * (int)gridDim.y, left = n - unit * V;
-    if (left <= 0) return;
-    for (long r = row; r < T; r += step) {
-        const unsigned char* src = codes + r * ldc;
-        const float s = mx_scale(scales[r * lds + unit / LANES]);      // of 255 an infinity, which makes the conversions' results NaN
+    for (Place at = walk_start(w); at.row < (unsigned)T; at = walk_next(w, at)) {
+        const int left = n - at.unit * V;
+        if (left <= 0) continue;
+        const unsigned char* src = codes + (long)at.row * ldc;
+        const float s = mx_scale(scales[(long)at.row * lds + at.unit / LANES]);      // of 255 an infinity, which makes the conversions' results NaN
         float v[V];
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) {
             float t[4];
             if constexpr (F == DQ_MXFP4) {
-                const unsigned word = V == 8 ? reinterpret_cast<const unsigned*>(src)[unit]
-                                             : (unsigned)reinterpret_cast<const unsigned short*>(src)[unit];
+                const unsigned word = V == 8 ? reinterpret_cast<const unsigned*>(src)[at.unit]
+                                             : (unsigned)reinterpret_cast<const unsigned short*>(src)[at.unit];
                 if (q == 0) mx_decode4<F, 0>(word, s, t); else mx_decode4<F, 1>(word, s, t);
             } else {
-                mx_decode4<F, 0>(reinterpret_cast<const unsigned*>(src)[unit * (V / 4) + q], s, t);
+                mx_decode4<F, 0>(reinterpret_cast<const unsigned*>(src)[at.unit * (V / 4) + q], s, t);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[4 * q + i] = t[i];
         }
-        store_piece(Y + r * ldy + (long)unit * V, left, v);
+        store_piece(Y + (long)at.row * ldy + (long)at.unit * V, left, v);
     }
 }
 
@@ -322,9 +320,10 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 // A workgroup takes the pieces of a long row 4 x 256 at a time, or those of four groups of rows of up to 1024 values (rg side by side), all four under
 // way together (10 problems of 2849 x 648: 53 us a row at a time, 37; but two rows of up to 2048 values each: 8192 x 2048 30 -> 34).  Bound by HBM: 8192 x
 // 4096 with a bf16 gradient, 201 MB, 35.3 us (5.7 TB/s); 64 problems of 2048 x 128 with an fp32 one, 134 MB, 26.7 us (5.0 TB/s).
+struct Rows { int upr, rg; };                      // pieces of a row; rows side by side
 template <int F, bool BF16OUT>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
-                                                           long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
+                                                           long lddy, double* __restrict__ partials, long sy, long sdy, Rows w) {
     constexpr int U = 4;
     __shared__ double tot[4];
     Y += (long)blockIdx.y * sy;
@@ -378,21 +377,21 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
     if (threadIdx.x == 0) partials[(long)blockIdx.y * gridDim.x + blockIdx.x] = ((tot[0] + tot[1]) + (tot[2] + tot[3])) / (double)n;
 }
 
-Walk make_walk(int n, int V) {
-    Walk w;
-    w.upr = (int)((n + 31L) / 32) * (32 / V);
-    w.rg = w.upr <= 128 ? 256 / w.upr : 1;
-    return w;
+int pieces_of(int n, int V) { return (int)((n + 31L) / 32) * (32 / V); }
+Rows make_rows(int n) {
+    const int upr = pieces_of(n, 4);
+    return Rows{upr, upr <= 128 ? 256 / upr : 1};
 }
-// at most 16384 workgroups, and each `batch` rows at a time where that leaves 2048, eight for every compute unit
-dim3 walk_grid(const Walk& w, int T, int batch) {
-    const long groups = ((long)T + w.rg - 1) / w.rg;
-    const long xt = w.rg > 1 ? 1 : (w.upr + 255) / 256;
-    long gy = (groups + batch - 1) / batch;
-    if (gy * xt < 2048) gy = (2048 + xt - 1) / xt;
-    if (gy * xt > 16384) gy = 16384 / xt;
-    gy = gy < 1 ? 1 : gy < groups ? gy : groups;
-    return dim3((unsigned)xt, (unsigned)gy);
+// at most 16384 workgroups, and each `batch` pieces a thread where that leaves 2048 of them, eight for every compute unit
+unsigned make_walk(int T, int n, int V, int batch, Walk& w) {
+    w.upr = pieces_of(n, V);
+    const long tiles = ((long)T * w.upr + 255) / 256;
+    long g = (tiles + batch - 1) / batch;
+    g = g < 2048 ? 2048 : g > 16384 ? 16384 : g;
+    g = g < tiles ? g : tiles;
+    w.rows = (unsigned)(256 * g / w.upr);
+    w.units = (int)(256 * g % w.upr);
+    return (unsigned)g;
 }
 
 // The norm's sum leaves past the caches where the input alone is more than the L2s hold (32 MB), so that little of it would be found there when it is
@@ -450,10 +449,11 @@ hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
 hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int n, int format, unsigned char* codes, long ldc, unsigned char* scales,
                               long lds, unsigned* flags, hipStream_t s) {
     if (T < 1 || n < 1) return hipSuccess;
-    const Walk w = make_walk(n, x_is_bf16 ? 8 : 4);
+    Walk w;
+    const unsigned grid = make_walk(T, n, x_is_bf16 ? 8 : 4, 4, w);
     const int nb = (int)((n + 31L) / 32);
 #define DQ_GO(IN, F)                                                                                                                                    \
-    hipLaunchKernelGGL((mx_quantize_kernel<IN, F>), walk_grid(w, T, 4), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, scales, lds, \
+    hipLaunchKernelGGL((mx_quantize_kernel<IN, F>), dim3(grid), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, scales, lds, \
                        w, flags)
     if (x_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
@@ -464,9 +464,10 @@ hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int
 hipError_t launch_mx_dequantize(int format, const unsigned char* codes, long ldc, const unsigned char* scales, long lds, int T, int n, void* Y,
                                 int y_is_bf16, long ldy, hipStream_t s) {
     if (T < 1 || n < 1) return hipSuccess;
-    const Walk w = make_walk(n, y_is_bf16 ? 8 : 4);
+    Walk w;
+    const unsigned grid = make_walk(T, n, y_is_bf16 ? 8 : 4, 1, w);
 #define DQ_GO(OUT, F)                                                                                                                        \
-    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), walk_grid(w, T, 1), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
+    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), dim3(grid), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
                        ldy, w)
     if (y_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
@@ -483,7 +484,7 @@ hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s) {
 // four row groups of short rows a workgroup; of the wider ones fewer where that would leave compute units without one (64 x 1000: 6.4 -> 5.2 us; not of
 // narrow ones, which come in batches: 64 problems of 2048 x 128 29 -> 39)
 int mx_objective_grid(int T, int n) {
-    const Walk w = make_walk(n, 4);
+    const Rows w = make_rows(n);
     const long groups = ((long)T + w.rg - 1) / w.rg, few = groups < 256 ? groups : 256, fourth = (groups + 3) / 4;
     const long g = w.upr > 256 ? groups : w.rg > 1 || fourth > few ? fourth : few;
     return (int)(g < 2048 ? g : 2048);
@@ -492,7 +493,7 @@ int mx_objective_grid(int T, int n) {
 hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy) {
     if (batch < 1 || T < 1) return hipSuccess;
-    const Walk w = make_walk(n, 4);
+    const Rows w = make_rows(n);
 #define DQ_GO(F, BF) \
     hipLaunchKernelGGL((mx_objective_kernel<F, BF>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, stride_dy, w)
     if (format == DQ_MXFP4) { if (dy_is_bf16) DQ_GO(DQ_MXFP4, true); else DQ_GO(DQ_MXFP4, false); }
