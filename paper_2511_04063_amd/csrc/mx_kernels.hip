@@ -320,54 +320,48 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 // A workgroup takes the pieces of a long row 4 x 256 at a time, or those of four groups of rows of up to 1024 values (rg side by side), all four under
 // way together (10 problems of 2849 x 648: 53 us a row at a time, 37; but two rows of up to 2048 values each: 8192 x 2048 30 -> 34).  Bound by HBM: 8192 x
 // 4096 with a bf16 gradient, 201 MB, 35.3 us (5.7 TB/s); 64 problems of 2048 x 128 with an fp32 one, 134 MB, 26.7 us (5.0 TB/s).
-struct Rows { int upr, rg; };                      // pieces of a row; rows side by side
 template <int F, bool BF16OUT>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
-                                                           long lddy, double* __restrict__ partials, long sy, long sdy, Rows w) {
+                                                           long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
     constexpr int U = 4;
     __shared__ double tot[4];
     Y += (long)blockIdx.y * sy;
     const float f = scale * 2.f / (float)n;
-    const bool side = w.upr <= 256;
-    const int r_in = side ? (int)threadIdx.x / w.upr : 0, u_in = side ? (int)threadIdx.x - r_in * w.upr : (int)threadIdx.x;
-    const long groups = ((long)T + w.rg - 1) / w.rg;
-    const long row_step = side ? (long)gridDim.x * w.rg : 0, hop = side ? U * (long)gridDim.x : gridDim.x;
     double acc = 0.0;
-    for (long group = blockIdx.x; group < groups; group += hop) {
-        for (int first = 0; first < w.upr; first += side ? w.upr : 256 * U) {
-            uint4 q[U];
-            bool in[U];
+    Place at = walk_start(w);
+    while (at.row < (unsigned)T) {
+        uint4 q[U];
+        Place p[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const long row = group * w.rg + r_in + k * row_step;
-                const int unit = side ? u_in : first + k * 256 + u_in;
-                in[k] = r_in < w.rg && unit < w.upr && row < T;
-                q[k] = load_whole<true>(Y + (in[k] ? row : 0) * ldy, in[k] ? unit * 4 : 0, n);
+        for (int k = 0; k < U; ++k) {
+            p[k] = at;
+            const bool in = at.row < (unsigned)T;
+            q[k] = load_whole<true>(Y + (long)(in ? at.row : 0u) * ldy, in ? at.unit * 4 : 0, n);
+            at = walk_next(w, at);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (p[k].row >= (unsigned)T) break;
+            const long row = p[k].row;
+            const int c = p[k].unit * 4;
+            finish_piece(q[k], Y + row * ldy, c, n);
+            float v[4], e[4];
+            unpack(q[k], v);
+            const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
+            unsigned code[1];
+            mx_encode<F, 4>(v, byte, code);
+            mx_decode4<F, 0>(code[0], mx_scale(byte), e);
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[i] = v[i] - e[i];          // NaN in a block of scale 255
+                ss += e[i] * e[i];
+                e[i] *= f;
             }
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                if (!in[k]) continue;
-                const long row = group * w.rg + r_in + k * row_step;
-                const int c = 4 * (side ? u_in : first + k * 256 + u_in);
-                finish_piece(q[k], Y + row * ldy, c, n);
-                float v[4], e[4];
-                unpack(q[k], v);
-                const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
-                unsigned code[1];
-                mx_encode<F, 4>(v, byte, code);
-                mx_decode4<F, 0>(code[0], mx_scale(byte), e);
-                float ss = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e[i] = v[i] - e[i];          // NaN in a block of scale 255
-                    ss += e[i] * e[i];
-                    e[i] *= f;
-                }
-                acc += (double)ss;
-                if (dYv != nullptr && c < n) {
-                    if constexpr (BF16OUT) store_piece<4>(static_cast<bf16_t*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
-                    else store_piece(static_cast<float*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
-                }
+            acc += (double)ss;
+            if (dYv != nullptr && c < n) {
+                if constexpr (BF16OUT) store_piece<4>(static_cast<bf16_t*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
+                else store_piece(static_cast<float*>(dYv) + (long)blockIdx.y * sdy + row * lddy + c, n - c, e);
             }
         }
     }
@@ -378,10 +372,6 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
 }
 
 int pieces_of(int n, int V) { return (int)((n + 31L) / 32) * (32 / V); }
-Rows make_rows(int n) {
-    const int upr = pieces_of(n, 4);
-    return Rows{upr, upr <= 128 ? 256 / upr : 1};
-}
 // at most 16384 workgroups, and each `batch` pieces a thread where that leaves 2048 of them, eight for every compute unit
 unsigned make_walk(int T, int n, int V, int batch, Walk& w) {
     w.upr = pieces_of(n, V);
@@ -481,19 +471,19 @@ hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s) {
     return m.format == DQ_MXFP4 ? norm_shape<float, DQ_MXFP4>(m, s) : norm_shape<float, DQ_MXFP8>(m, s);
 }
 
-// four row groups of short rows a workgroup; of the wider ones fewer where that would leave compute units without one (64 x 1000: 6.4 -> 5.2 us; not of
-// narrow ones, which come in batches: 64 problems of 2048 x 128 29 -> 39)
+// four pieces a thread
 int mx_objective_grid(int T, int n) {
-    const Rows w = make_rows(n);
-    const long groups = ((long)T + w.rg - 1) / w.rg, few = groups < 256 ? groups : 256, fourth = (groups + 3) / 4;
-    const long g = w.upr > 256 ? groups : w.rg > 1 || fourth > few ? fourth : few;
+    const long tiles = ((long)T * pieces_of(n, 4) + 255) / 256, g = (tiles + 3) / 4;
     return (int)(g < 2048 ? g : 2048);
 }
 
 hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy) {
     if (batch < 1 || T < 1) return hipSuccess;
-    const Rows w = make_rows(n);
+    Walk w;
+    w.upr = pieces_of(n, 4);
+    w.rows = (unsigned)(256L * grid / w.upr);
+    w.units = (int)(256L * grid % w.upr);
 #define DQ_GO(F, BF) \
     hipLaunchKernelGGL((mx_objective_kernel<F, BF>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, stride_dy, w)
     if (format == DQ_MXFP4) { if (dy_is_bf16) DQ_GO(DQ_MXFP4, true); else DQ_GO(DQ_MXFP4, false); }
