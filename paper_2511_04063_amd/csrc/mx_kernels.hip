@@ -30,38 +30,37 @@ __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
         v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-// The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  Without a branch: in place of a piece
-// that is not whole the row's last V values are read, and shifted to their place afterwards (the norm of 8192 x 1100 in bf16: 20.6 us with such values
-// read one by one, 17.1); value by value only of rows shorter than a piece.
+// The piece of V values at column c of a row of n; what lies behind the row's end reads as zero and is not touched.  In place of a piece that is not
+// whole the row's last V values are read, and shifted to their place afterwards (the norm of 8192 x 1100 in bf16: 20.6 us with such values read one by one,
+// 17.1).  TINY: rows shorter than a piece, value by value.
 // STREAM: past the caches, for what is read once by a kernel that writes less than it reads (quantiser 8192 x 8192 42 -> 34 us, objective 8192 x 4096
 // 39 -> 35; the norm, which writes as much, 50 -> 52).
-template <bool STREAM, class T>
+template <bool STREAM, bool TINY, class T>
 __device__ __forceinline__ uint4 load_whole(const T* row, int c, int n) {
-    if (n < Piece<T>::V) return make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (TINY) return make_uint4(0u, 0u, 0u, 0u);
     const typename Piece<T>::Anywhere* at = reinterpret_cast<const typename Piece<T>::Anywhere*>(row + (c + Piece<T>::V <= n ? c : n - Piece<T>::V));
     const u32x4 q = STREAM ? __builtin_nontemporal_load(at) : *at;
     return make_uint4(q.x, q.y, q.z, q.w);
 }
-template <class T>
+template <bool TINY, class T>
 __device__ __forceinline__ void finish_piece(uint4& q, const T* row, int c, int n) {
     constexpr int V = Piece<T>::V, BITS = 128 / V;
-    if (n >= V) {
-        const int over = c + V - n, by = BITS * over;        // values behind the end
-        if (over > 0) {
-            const unsigned long long lo = (unsigned long long)q.y << 32 | q.x, hi = (unsigned long long)q.w << 32 | q.z;
-            const unsigned long long low = by < 64 ? lo >> by | hi << (64 - by) : by < 128 ? hi >> (by - 64) : 0ull, high = by < 64 ? hi >> by : 0ull;
-            q = make_uint4((unsigned)low, (unsigned)(low >> 32), (unsigned)high, (unsigned)(high >> 32));
-        }
-        return;
-    }
-    unsigned w[4] = {0u, 0u, 0u, 0u};
+    const int over = c + V - n;        // values behind the end
+    if constexpr (TINY) {
+        unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < V - 1; ++i)
-        if (c + i < n) {
-            if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
-            else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
-        }
-    q = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int i = 0; i < V; ++i)
+            if (c + i < n) {
+                if constexpr (V == 4) w[i] = __float_as_uint(row[c + i]);
+                else w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+            }
+        q = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (over > 0) {
+        const int by = BITS * over;
+        const unsigned long long lo = (unsigned long long)q.y << 32 | q.x, hi = (unsigned long long)q.w << 32 | q.z;
+        const unsigned long long low = by < 64 ? lo >> by | hi << (64 - by) : by < 128 ? hi >> (by - 64) : 0ull, high = by < 64 ? hi >> by : 0ull;
+        q = make_uint4((unsigned)low, (unsigned)(low >> 32), (unsigned)high, (unsigned)(high >> 32));
+    }
 }
 __device__ __forceinline__ void store_piece(float* dst, int left, const float (&v)[4]) {
     if (left >= 4) {
@@ -122,21 +121,23 @@ __device__ __forceinline__ void put_blocks(const float (&v)[NV], int unit, int n
     }
 }
 
-// Threads over all pieces of all rows, `upr` a row: a thread's next piece is 256 times the grid further on, `rows` rows and `units` pieces.
-struct Walk { int upr; unsigned rows; int units; };
+// Threads over all pieces of all rows, `upr` a row: a workgroup takes `run` times 256 neighbouring ones, then as many 256 `run` times the grid further
+// on (objective 8192 x 4096, bf16 gradient: 40.7 us with 256 at a time, 34.1).  A step of a thread is so many rows and pieces.
+struct Step { unsigned rows; int units; };
+struct Walk { int upr, run; Step near, far; };
 struct Place { unsigned row; int unit; };
 __device__ __forceinline__ Place walk_start(const Walk& w) {
-    const unsigned item = blockIdx.x * 256 + threadIdx.x, row = item / (unsigned)w.upr;
+    const unsigned item = blockIdx.x * (256u * w.run) + threadIdx.x, row = item / (unsigned)w.upr;
     return Place{row, (int)(item - row * (unsigned)w.upr)};
 }
-__device__ __forceinline__ Place walk_next(const Walk& w, const Place& at) {
-    const int unit = at.unit + w.units;
-    return unit < w.upr ? Place{at.row + w.rows, unit} : Place{at.row + w.rows + 1, unit - w.upr};
+__device__ __forceinline__ Place walk_next(const Walk& w, const Place& at, const Step& s) {
+    const int unit = at.unit + s.units;
+    return unit < w.upr ? Place{at.row + s.rows, unit} : Place{at.row + s.rows + 1, unit - w.upr};
 }
 
-// Bound by HBM; U pieces of a thread under way at a time, or their latency shows (8192 x 8192 bf16 to 4 bits, 170 MB, 42 -> 34 us with the loads past
-// the caches: 5.0 TB/s, a large copy reaches 5.3; 333 x 2890, 5 MB: 3.7 us, 2 of them a kernel's own).
-template <class IN, int F>
+// Bound by HBM; U pieces of a thread under way at a time, or their latency shows (8192 x 8192 bf16 to 4 bits, 170 MB, 30.5 us: 5.6 TB/s, a
+// large copy reaches 5.3; 333 x 2890, 5 MB: 3.5 us, 2 of them a kernel's own).
+template <class IN, int F, bool TINY>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__ X, long ldx, int T, int n, int nb, unsigned char* __restrict__ codes,
                                                           long ldc, unsigned char* __restrict__ scales, long lds, Walk w, unsigned* flags) {
     constexpr int V = Piece<IN>::V, U = 4;
@@ -148,13 +149,13 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const IN* __restrict__
         for (int k = 0; k < U; ++k) {
             p[k] = at;
             const bool in = at.row < (unsigned)T;
-            q[k] = load_whole<true>(X + (long)(in ? at.row : 0u) * ldx, in ? at.unit * V : 0, n);
-            at = walk_next(w, at);
+            q[k] = load_whole<true, TINY>(X + (long)(in ? at.row : 0u) * ldx, in ? at.unit * V : 0, n);
+            at = walk_next(w, at, k < U - 1 ? w.near : w.far);
         }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (p[k].row >= (unsigned)T) break;
-            finish_piece(q[k], X + (long)p[k].row * ldx, p[k].unit * V, n);
+            finish_piece<TINY>(q[k], X + (long)p[k].row * ldx, p[k].unit * V, n);
             float v[V];
             unpack(q[k], v);
             put_blocks<F, V>(v, p[k].unit, nb, codes + (long)p[k].row * ldc, scales + (long)p[k].row * lds, flags);
@@ -168,7 +169,7 @@ template <class OUT, int F>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const unsigned char* __restrict__ codes, long ldc, const unsigned char* __restrict__ scales,
                                                             long lds, int T, int n, OUT* __restrict__ Y, long ldy, Walk w) {
     constexpr int V = Piece<OUT>::V, LANES = 32 / V;
-    for (Place at = walk_start(w); at.row < (unsigned)T; at = walk_next(w, at)) {
+    for (Place at = walk_start(w); at.row < (unsigned)T; at = walk_next(w, at, w.far)) {
         const int left = n - at.unit * V;
         if (left <= 0) continue;
         const unsigned char* src = codes + (long)at.row * ldc;
@@ -225,7 +226,7 @@ __device__ __forceinline__ void store_sum(T* to, const uint4& q) {
 // A row is read once and stays in registers, all of its loads under way together.  Bound by HBM: 8192 x 4096 bf16 with the residual to
 // 8 bits, 235 MB, 36.5 us in a row (6.4 TB/s) and 45 where what reads the codes runs between (5.2); one token of 4096 2.6 us, a kernel of no
 // work takes 2.
-template <class IN, int F, int P, int TPR, bool PAST>
+template <class IN, int F, int P, int TPR, bool PAST, bool TINY>
 __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx, const IN* res, long ldr, IN* H, long ldh, const float* __restrict__ gain,
                                                           float eps, int T, int n, int nb, unsigned char* __restrict__ codes, long ldc,
                                                           unsigned char* __restrict__ scales, long lds, unsigned* flags) {
@@ -236,15 +237,15 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
     const bool live = row < T;
     uint4 q[P], z[P];
 #pragma unroll
-    for (int p = 0; p < P; ++p) q[p] = load_whole<false>(X + at * ldx, (p * TPR + t) * V, n);
+    for (int p = 0; p < P; ++p) q[p] = load_whole<false, TINY>(X + at * ldx, (p * TPR + t) * V, n);
     if (res != nullptr) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) z[p] = load_whole<false>(res + at * ldr, (p * TPR + t) * V, n);
+        for (int p = 0; p < P; ++p) z[p] = load_whole<false, TINY>(res + at * ldr, (p * TPR + t) * V, n);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int c = (p * TPR + t) * V;
-            finish_piece(q[p], X + at * ldx, c, n);
-            finish_piece(z[p], res + at * ldr, c, n);
+            finish_piece<TINY>(q[p], X + at * ldx, c, n);
+            finish_piece<TINY>(z[p], res + at * ldr, c, n);
             float h[V], r[V];
             unpack(q[p], h);
             unpack(z[p], r);
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
         }
     } else {
 #pragma unroll
-        for (int p = 0; p < P; ++p) finish_piece(q[p], X + at * ldx, (p * TPR + t) * V, n);
+        for (int p = 0; p < P; ++p) finish_piece<TINY>(q[p], X + at * ldx, (p * TPR + t) * V, n);
     }
     double ss = 0.0;
 #pragma unroll
@@ -297,8 +298,8 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
             float g[V];
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
-                uint4 u = load_whole<false>(gain, c + i, n);
-                finish_piece(u, gain, c + i, n);
+                uint4 u = load_whole<false, TINY>(gain, c + i, n);
+                finish_piece<TINY>(u, gain, c + i, n);
                 float g4[4];
                 unpack(u, g4);
 #pragma unroll
@@ -317,10 +318,9 @@ __global__ __launch_bounds__(256) void mx_rms_norm_kernel(const IN* X, long ldx,
 // Squared error of the MX quantiser and its derivative:  loss_t = (1/n) sum_i (y_i - yhat_i)^2,  dY_i = c (2/n) (y_i - yhat_i).  yhat is
 // constant around almost every y (the scale is a power of two), so this is the derivative wherever there is one.
 //
-// A workgroup takes the pieces of a long row 4 x 256 at a time, or those of four groups of rows of up to 1024 values (rg side by side), all four under
-// way together (10 problems of 2849 x 648: 53 us a row at a time, 37; but two rows of up to 2048 values each: 8192 x 2048 30 -> 34).  Bound by HBM: 8192 x
-// 4096 with a bf16 gradient, 201 MB, 35.3 us (5.7 TB/s); 64 problems of 2048 x 128 with an fp32 one, 134 MB, 26.7 us (5.0 TB/s).
-template <int F, bool BF16OUT>
+// Bound by HBM: 8192 x 4096 with a bf16 gradient, 201 MB, 34.1 us (5.9 TB/s); 64 problems of 2048 x 128 with an fp32 one, 134 MB, 24.9 us (5.4 TB/s); 10
+// of 2849 x 648 32 us (53 with a row a workgroup at a time).
+template <int F, bool BF16OUT, bool TINY>
 __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restrict__ Y, long ldy, int T, int n, float scale, void* __restrict__ dYv,
                                                            long lddy, double* __restrict__ partials, long sy, long sdy, Walk w) {
     constexpr int U = 4;
@@ -336,15 +336,15 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
         for (int k = 0; k < U; ++k) {
             p[k] = at;
             const bool in = at.row < (unsigned)T;
-            q[k] = load_whole<true>(Y + (long)(in ? at.row : 0u) * ldy, in ? at.unit * 4 : 0, n);
-            at = walk_next(w, at);
+            q[k] = load_whole<true, TINY>(Y + (long)(in ? at.row : 0u) * ldy, in ? at.unit * 4 : 0, n);
+            at = walk_next(w, at, k < U - 1 ? w.near : w.far);
         }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (p[k].row >= (unsigned)T) break;
             const long row = p[k].row;
             const int c = p[k].unit * 4;
-            finish_piece(q[k], Y + row * ldy, c, n);
+            finish_piece<TINY>(q[k], Y + row * ldy, c, n);
             float v[4], e[4];
             unpack(q[k], v);
             const unsigned byte = mx_scale_byte<F>(mx_group_max<8>(piece_top(v)));
@@ -372,16 +372,18 @@ __global__ __launch_bounds__(256) void mx_objective_kernel(const float* __restri
 }
 
 int pieces_of(int n, int V) { return (int)((n + 31L) / 32) * (32 / V); }
+// neighbouring pieces only where every workgroup gets `batch` times 256 of them
+Walk make_walk(int T, int upr, int batch, long grid) {
+    const int run = (long)T * upr >= 256 * batch * grid ? batch : 1;
+    const long near = run > 1 ? 256 : 256 * grid, far = run > 1 ? 256 * (batch * grid - (batch - 1)) : 256 * grid;
+    return Walk{upr, run, {(unsigned)(near / upr), (int)(near % upr)}, {(unsigned)(far / upr), (int)(far % upr)}};
+}
 // at most 16384 workgroups, and each `batch` pieces a thread where that leaves 2048 of them, eight for every compute unit
-unsigned make_walk(int T, int n, int V, int batch, Walk& w) {
-    w.upr = pieces_of(n, V);
-    const long tiles = ((long)T * w.upr + 255) / 256;
+long walk_grid(int T, int upr, int batch) {
+    const long tiles = ((long)T * upr + 255) / 256;
     long g = (tiles + batch - 1) / batch;
     g = g < 2048 ? 2048 : g > 16384 ? 16384 : g;
-    g = g < tiles ? g : tiles;
-    w.rows = (unsigned)(256 * g / w.upr);
-    w.units = (int)(256 * g % w.upr);
-    return (unsigned)g;
+    return g < tiles ? g : tiles;
 }
 
 // The norm's sum leaves past the caches where the input alone is more than the L2s hold (32 MB), so that little of it would be found there when it is
@@ -389,7 +391,7 @@ unsigned make_walk(int T, int n, int V, int batch, Walk& w) {
 // itself gains 34 -> 32 us at 8192 x 8192 by codes past them, and what reads those next loses 7).
 bool past_caches(int T, int n, int is_bf16) { return (long)T * n * (is_bf16 ? 2 : 4) > (32L << 20); }
 
-template <class IN, int F, int P, int TPR>
+template <class IN, int F, int P, int TPR, bool TINY = false>
 hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
     constexpr int ROWS = 256 / TPR;
     const bool past = past_caches(m.T, m.n, m.x_is_bf16);
@@ -399,7 +401,7 @@ hipError_t norm_launch(const MxNorm& m, hipStream_t s) {
         const IN *X = static_cast<const IN*>(m.X) + first * m.ldx, *res = m.res != nullptr ? static_cast<const IN*>(m.res) + first * m.ldr : nullptr;
         IN* H = m.H != nullptr ? static_cast<IN*>(m.H) + first * m.ldh : nullptr;
 #define DQ_GO(PAST)                                                                                                                          \
-    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, PAST>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), 0, s, X, m.ldx, res, \
+    hipLaunchKernelGGL((mx_rms_norm_kernel<IN, F, P, TPR, PAST, TINY>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), 0, s, X, m.ldx, res, \
                        m.ldr, H, m.ldh, m.gain, m.eps, (int)rows, m.n, (m.n + 31) / 32, m.codes + first * m.ldc, m.ldc,                       \
                        m.scales + first * m.lds, m.lds, m.flags)
         if (past) DQ_GO(true); else DQ_GO(false);
@@ -431,6 +433,7 @@ hipError_t norm_pieces(const MxNorm& m, hipStream_t s) {
 template <class IN, int F>
 hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
     constexpr int V = Piece<IN>::V;
+    if (m.n < V) return norm_launch<IN, F, 1, 64, true>(m, s);
     return m.n <= 64 * V || (m.n <= 64 * V * (V == 8 ? 4 : 5) && m.T > 1024) ? norm_pieces<IN, F, 64>(m, s) : norm_pieces<IN, F, 256>(m, s);
 }
 
@@ -439,14 +442,17 @@ hipError_t norm_shape(const MxNorm& m, hipStream_t s) {
 hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int n, int format, unsigned char* codes, long ldc, unsigned char* scales,
                               long lds, unsigned* flags, hipStream_t s) {
     if (T < 1 || n < 1) return hipSuccess;
-    Walk w;
-    const unsigned grid = make_walk(T, n, x_is_bf16 ? 8 : 4, 4, w);
+    const int V = x_is_bf16 ? 8 : 4, upr = pieces_of(n, V);
+    const long grid = walk_grid(T, upr, 4);
+    const Walk w = make_walk(T, upr, 4, grid);
     const int nb = (int)((n + 31L) / 32);
-#define DQ_GO(IN, F)                                                                                                                                    \
-    hipLaunchKernelGGL((mx_quantize_kernel<IN, F>), dim3(grid), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, ldc, scales, lds, \
-                       w, flags)
-    if (x_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
-    else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
+#define DQ_GO(IN, F, TINY)                                                                                                                      \
+    hipLaunchKernelGGL((mx_quantize_kernel<IN, F, TINY>), dim3((unsigned)grid), dim3(256), 0, s, static_cast<const IN*>(X), ldx, T, n, nb, codes, \
+                       ldc, scales, lds, w, flags)
+#define DQ_FORMAT(IN, TINY) do { if (format == DQ_MXFP4) DQ_GO(IN, DQ_MXFP4, TINY); else DQ_GO(IN, DQ_MXFP8, TINY); } while (0)
+    if (x_is_bf16) { if (n < V) DQ_FORMAT(bf16_t, true); else DQ_FORMAT(bf16_t, false); }
+    else { if (n < V) DQ_FORMAT(float, true); else DQ_FORMAT(float, false); }
+#undef DQ_FORMAT
 #undef DQ_GO
     return hipGetLastError();
 }
@@ -454,10 +460,11 @@ hipError_t launch_mx_quantize(const void* X, int x_is_bf16, long ldx, int T, int
 hipError_t launch_mx_dequantize(int format, const unsigned char* codes, long ldc, const unsigned char* scales, long lds, int T, int n, void* Y,
                                 int y_is_bf16, long ldy, hipStream_t s) {
     if (T < 1 || n < 1) return hipSuccess;
-    Walk w;
-    const unsigned grid = make_walk(T, n, y_is_bf16 ? 8 : 4, 1, w);
+    const int upr = pieces_of(n, y_is_bf16 ? 8 : 4);
+    const long grid = walk_grid(T, upr, 1);
+    const Walk w = make_walk(T, upr, 1, grid);
 #define DQ_GO(OUT, F)                                                                                                                        \
-    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), dim3(grid), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
+    hipLaunchKernelGGL((mx_dequantize_kernel<OUT, F>), dim3((unsigned)grid), dim3(256), 0, s, codes, ldc, scales, lds, T, n, static_cast<OUT*>(Y), \
                        ldy, w)
     if (y_is_bf16) { if (format == DQ_MXFP4) DQ_GO(bf16_t, DQ_MXFP4); else DQ_GO(bf16_t, DQ_MXFP8); }
     else { if (format == DQ_MXFP4) DQ_GO(float, DQ_MXFP4); else DQ_GO(float, DQ_MXFP8); }
@@ -471,23 +478,23 @@ hipError_t launch_mx_rms_norm(const MxNorm& m, hipStream_t s) {
     return m.format == DQ_MXFP4 ? norm_shape<float, DQ_MXFP4>(m, s) : norm_shape<float, DQ_MXFP8>(m, s);
 }
 
-// four pieces a thread
+// four pieces a thread, fewer in a small problem
 int mx_objective_grid(int T, int n) {
-    const long tiles = ((long)T * pieces_of(n, 4) + 255) / 256, g = (tiles + 3) / 4;
-    return (int)(g < 2048 ? g : 2048);
+    const long tiles = ((long)T * pieces_of(n, 4) + 255) / 256, few = tiles < 32 ? tiles : 32, g = (tiles + 3) / 4;
+    return (int)(g < few ? few : g < 2048 ? g : 2048);
 }
 
 hipError_t launch_mx_objective(int format, const float* Y, long ldy, int T, int n, float scale, void* dY, int dy_is_bf16, long lddy, double* partials,
                                int grid, hipStream_t s, int batch, long stride_y, long stride_dy) {
     if (batch < 1 || T < 1) return hipSuccess;
-    Walk w;
-    w.upr = pieces_of(n, 4);
-    w.rows = (unsigned)(256L * grid / w.upr);
-    w.units = (int)(256L * grid % w.upr);
-#define DQ_GO(F, BF) \
-    hipLaunchKernelGGL((mx_objective_kernel<F, BF>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, stride_dy, w)
-    if (format == DQ_MXFP4) { if (dy_is_bf16) DQ_GO(DQ_MXFP4, true); else DQ_GO(DQ_MXFP4, false); }
-    else { if (dy_is_bf16) DQ_GO(DQ_MXFP8, true); else DQ_GO(DQ_MXFP8, false); }
+    const Walk w = make_walk(T, pieces_of(n, 4), 4, grid);
+#define DQ_GO(F, BF, TINY)                                                                                                                          \
+    hipLaunchKernelGGL((mx_objective_kernel<F, BF, TINY>), dim3(grid, batch), dim3(256), 0, s, Y, ldy, T, n, scale, dY, lddy, partials, stride_y, \
+                       stride_dy, w)
+#define DQ_TYPE(F, TINY) do { if (dy_is_bf16) DQ_GO(F, true, TINY); else DQ_GO(F, false, TINY); } while (0)
+    if (format == DQ_MXFP4) { if (n < 4) DQ_TYPE(DQ_MXFP4, true); else DQ_TYPE(DQ_MXFP4, false); }
+    else { if (n < 4) DQ_TYPE(DQ_MXFP8, true); else DQ_TYPE(DQ_MXFP8, false); }
+#undef DQ_TYPE
 #undef DQ_GO
     return hipGetLastError();
 }

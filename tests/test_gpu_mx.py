@@ -66,7 +66,7 @@ def check_stored(codes, scales, ref_codes, ref_scales, fmt, n):
     assert np.array_equal(mx.unpack(got_c[:, :cb], fmt), ref_codes)
 
 
-SHAPES = [(1, 1), (1, 32), (2, 31), (7, 33), (5, 100), (64, 128), (9, 515), (33, 1000), (3, 2890), (17, 4096), (6, 8200), (300, 40), (4100, 8)]
+SHAPES = [(1, 1), (5, 3), (9, 5), (70, 7), (1, 32), (2, 31), (7, 33), (5, 100), (64, 128), (9, 515), (33, 1000), (3, 2890), (17, 4096), (6, 8200), (300, 40), (4100, 8)]
 
 
 @pytest.mark.parametrize("T,n", SHAPES)
@@ -162,7 +162,7 @@ def test_large_inputs_give_the_codes_of_their_parts(ctx, fmt, xdt):
 
 
 # ----------------------------------------------------------------------------------- norm
-NORM_SHAPES = [(1, 1), (3, 33), (130, 40), (5, 300), (4, 512), (9, 513), (6, 1000), (3, 1024), (5, 2048), (2, 2890), (1, 4096), (7, 4100), (9, 5004), (2, 5120), (5, 5800), (4, 6145), (3, 8192), (0, 64),
+NORM_SHAPES = [(1, 1), (5, 3), (9, 5), (3, 7), (3, 33), (130, 40), (5, 300), (4, 512), (9, 513), (6, 1000), (3, 1024), (5, 2048), (2, 2890), (1, 4096), (7, 4100), (9, 5004), (2, 5120), (5, 5800), (4, 6145), (3, 8192), (0, 64),
                (1030, 700), (1025, 1101), (1029, 1279), (1026, 2046), (1500, 129)]
 
 
@@ -259,7 +259,7 @@ def test_objective_of_many_rows_and_of_many_problems(ctx):
             assert abs(loss[i].item() - ref_loss) <= 8 * 2.0 ** -24 * ref_loss
 
 
-@pytest.mark.parametrize("b,T,n", [(1, 1, 1), (1, 5, 33), (3, 45, 640), (1, 37, 101), (64, 9, 128), (2, 300, 80), (1, 19, 1500), (1, 9, 4096), (1, 5, 8192), (1, 7, 5001), (1, 9001, 530)])
+@pytest.mark.parametrize("b,T,n", [(1, 1, 1), (2, 7, 3), (1, 9, 6), (1, 5, 33), (3, 45, 640), (1, 37, 101), (64, 9, 128), (2, 300, 80), (1, 19, 1500), (1, 9, 4096), (1, 5, 8192), (1, 7, 5001), (1, 9001, 530)])
 @pytest.mark.parametrize("grad", [B.DQ_F32, B.DQ_BF16])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_objective(ctx, fmt, grad, b, T, n):
