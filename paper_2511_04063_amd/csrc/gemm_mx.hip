@@ -8,7 +8,10 @@
 // Eight products at a time (k = 8 j .. 8 j + 7) are summed inside the instruction with about 14 bits below the largest of them when an operand has 8-bit
 // codes: normal values come out with an error of 1.5e-5 of the result's norm (8 x 8 bits) or 4e-6 (8 x 4), far below a bf16 result's rounding;
 // 4 x 4 bits show none.  A caller who asks for fp32 gets fp32 sums: there 8-bit operands (and what they meet) go to the bf16 matrix cores,
-// value times scale being exact in bf16.
+// as value times scale times 2^20, which bf16 holds exactly for scales below 2^17 (2^-127 2^-9 2^20 is a normal number; 2^31 products of two largest
+// ones stay below 2^121), and the sums lose the 2^40 at the end.  A wavefront that meets a larger scale, which takes values of 2^19 (4 bits) or 2^25 and
+// more, forms its sums again: by the scaled instruction, which holds any scales, with all but one of each eight codes of A masked, eight times, so that
+// nothing is lost (8192^3 of 8 x 8 bits 870 us, with large scales everywhere 5.8 ms).
 #include "dq_mx.h"
 
 namespace dq {
@@ -57,10 +60,18 @@ __device__ __forceinline__ Codes<F> load_codes(const unsigned char* row, int ste
     return c;
 }
 
-// codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale, in bf16; scale 255 makes the conversions' results NaN
+constexpr int kLift = 20;                                    // the fp32 route's values are 2^20 times what they stand for
+constexpr float kLower = 1.f / (1L << 2 * kLift);
+constexpr unsigned kLargeScale = 127u + 17u;                 // scale bytes from here on, but 255, are too large for it
+// nonzero where one of the four scale bytes of a word is: its highest bit and one of the next three, and not all of them
+__device__ __forceinline__ unsigned large_scales(unsigned w) { return w & (w << 1 | w << 2 | w << 3) & ~((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ bool large_scale(unsigned byte) { return byte - kLargeScale < 255u - kLargeScale; }
+static_assert(kLargeScale == 0x90u, "large_scales looks at these bits");
+
+// codes [8 j, 8 j + 8) of this lane's 32 (loaded WIDE), times their scale and 2^20, in bf16; scale 255 makes the conversions' results NaN
 template <int F, int J>
 __device__ __forceinline__ bf16x8 values8(const Codes<F>& c, unsigned byte) {
-    const float s = mx_scale(byte);
+    const float s = __uint_as_float(((byte < 255u - kLift ? byte : 255u - kLift) + kLift) << 23);
     unsigned w[4];
     if constexpr (F == DQ_MXFP4) {
         const unsigned u = (unsigned)c.a[J];
@@ -87,6 +98,38 @@ __device__ __forceinline__ f32x4 mfma_values(const Codes<FA>& a, const Codes<FB>
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values8<FA, 1>(a, sa), values8<FB, 1>(b, sb), c, 0, 0, 0);
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values8<FA, 2>(a, sa), values8<FB, 2>(b, sb), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(values8<FA, 3>(a, sa), values8<FB, 3>(b, sb), c, 0, 0, 0);
+}
+
+// of each eight neighbouring codes the j-th alone
+template <int F>
+__device__ __forceinline__ Codes<F> one_of_eight(Codes<F> c, int j) {
+    if constexpr (F == DQ_MXFP4) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) c.a[w] &= (int)(0xfu << (4 * j));
+    } else {
+        const unsigned m[2] = {j < 4 ? 0xffu << (8 * j) : 0u, j < 4 ? 0u : 0xffu << (8 * (j - 4))};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            c.a[w] &= (int)m[w & 1];
+            c.b[w] &= (int)m[w & 1];
+        }
+    }
+    return c;
+}
+
+// This lane's codes and scale of 64 of a row, as the 32 x 32 x 64 instruction takes them; as load_codes
+template <int F>
+__device__ __forceinline__ Codes<F> load_codes64(const unsigned char* row, int step, int q, int nb) {
+    const i32x4 zero = {0, 0, 0, 0};
+    const unsigned char* p = row + (long)step * (kStepBytes<F> / 2) + 16 * q;
+    Codes<F> c;
+    if constexpr (F == DQ_MXFP4) {
+        c.a = 2 * step + q < nb ? *reinterpret_cast<const i32x4*>(p) : zero;
+    } else {
+        c.a = *reinterpret_cast<const i32x4*>(p);
+        c.b = 2 * step + 1 < nb ? *reinterpret_cast<const i32x4*>(p + 32) : zero;
+    }
+    return c;
 }
 
 template <class OUT>
@@ -136,6 +179,7 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool large = false;
     for (int piece = wave; 16 * piece < nb; piece += 8) {
         Codes<FA> a[4][MT];
         Codes<FB> b[4][NT];
@@ -160,10 +204,35 @@ __global__ __launch_bounds__(512) void gemm_mx_direct_kernel(GemmMx g, int tiles
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     const unsigned xb = in ? (unsigned)eb[j][t] >> (8 * q) : 0u;
-                    if constexpr (EXACT) acc[i][j] = mfma_values<FB, FA>(b[t][j], a[t][i], acc[i][j], xb & 255u, xa & 255u);
-                    else acc[i][j] = mfma_mx<FB, FA>(b[t][j], a[t][i], acc[i][j], (int)xb, (int)xa);
+                    if constexpr (EXACT) {
+                        large |= large_scale(xa & 255u) || large_scale(xb & 255u);
+                        acc[i][j] = mfma_values<FB, FA>(b[t][j], a[t][i], acc[i][j], xb & 255u, xa & 255u);
+                    } else acc[i][j] = mfma_mx<FB, FA>(b[t][j], a[t][i], acc[i][j], (int)xb, (int)xa);
                 }
             }
+        }
+    }
+    if constexpr (EXACT) {
+        const bool again = __any(large);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] *= kLower;
+        if (again) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    f32x4 c = {0.f, 0.f, 0.f, 0.f};
+                    for (int step = 4 * wave; 4 * step < nb; step += step % 4 == 3 ? 29 : 1) {
+                        const int block = 4 * step + q;
+                        const int xa = block < nb ? sa[i][block] : 0, xb = block < nb ? sb[j][block] : 0;
+                        const Codes<FA> a = load_codes<FA, false>(pa[i], step, q, nb);
+                        const Codes<FB> b = load_codes<FB, false>(pb[j], step, q, nb);
+                        for (int k = 0; k < 8; ++k) c = mfma_mx<FB, FA>(b, one_of_eight<FA>(a, k), c, xb, xa);
+                    }
+                    acc[i][j] = c;
+                }
         }
     }
 #pragma unroll
@@ -390,6 +459,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
     constexpr int FR = MI + NI;
     i32x4 raw[(FR + 1) / 2];
     int sc[FR][2];
+    unsigned large = 0u;
     auto frag_row = [&](int k) { return k < MI ? wm + 32 * k : S::TM + wn + 32 * (k - MI); };
     auto read_scales = [&](int chunk) {
         const unsigned char* at = smem + kScalesAt + (S::kScaleSets == 1 ? 0 : (chunk & 1) * S::kScaleBytes);
@@ -411,6 +481,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const unsigned lo = (unsigned)raw[k / 2][2 * w] & keep[2 * w], hi = (unsigned)raw[k / 2][2 * w + 1] & keep[2 * w + 1];
+                if constexpr (EXACT) large |= large_scales(lo) | large_scales(hi);
                 const unsigned even = __builtin_amdgcn_perm(hi, lo, 0x06040200u), odd = __builtin_amdgcn_perm(hi, lo, 0x07050301u);
                 const auto x = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
                 sc[k][w] = (int)x[0];
@@ -500,6 +571,37 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS) void gemm_mx_tile_kernel(GemmM
         step(std::integral_constant<int, 7>{}, stage + 7 / SUBS);
     }
     arrived<0>();        // nothing may still be on its way into LDS when the workgroup ends
+
+    if constexpr (EXACT) {
+        const bool again = __any(large != 0u);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] *= kLower;
+        if (again) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const int m = m0 + wm + 32 * i + r, n = n0 + wn + 32 * j + r;
+                    const long row_a = m < g.M ? m : g.M - 1, row_b = n < g.N ? n : g.N - 1;
+                    const unsigned char *pa = g.A + row_a * g.lda, *pb = g.B + row_b * g.ldb, *sa = g.As + row_a * g.ldas, *sb = g.Bs + row_b * g.ldbs;
+                    f32x16 c;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) c[v] = 0.f;
+                    for (int step = 8 * group; 2 * step < nb; step += step % 8 == 7 ? 8 * GROUPS - 7 : 1) {
+                        const int block = 2 * step + q;
+                        const int xa = block < nb ? sa[block] : 0, xb = block < nb ? sb[block] : 0;
+                        const Codes<FA> a = load_codes64<FA>(pa, step, q, nb);
+                        const Codes<FB> b = load_codes64<FB>(pb, step, q, nb);
+                        for (int k = 0; k < 8; ++k)
+                            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand<FB>(b), operand<FA>(one_of_eight<FA>(a, k)), c, kMfmaFormat<FB>,
+                                                                                kMfmaFormat<FA>, 0, xb, 0, xa);
+                    }
+                    acc[i][j] = c;
+                }
+        }
+    }
 
     // the groups' sums, added in order
     if constexpr (GROUPS > 1) {

@@ -9,7 +9,9 @@ torch = pytest.importorskip("torch")
 
 from oracle import mx_oracle as mx  # noqa: E402
 from paper_2511_04063_amd import binding as B  # noqa: E402
-from test_gpu_mx import TYPES, rng, up  # noqa: E402
+from test_gpu_mx import TYPES, random_matrix, rng, stored, up  # noqa: E402
+
+PAIRS = [(0, 0), (1, 0), (0, 1), (1, 1)]
 
 
 @pytest.fixture(scope="module")
@@ -49,3 +51,75 @@ def test_objective_whose_squares_leave_fp32(ctx, obj, fmt, grad, where):
     assert abs(loss.item() - ref_loss) <= 8 * 2.0 ** -24 * ref_loss
     assert (np.abs(buf.double().cpu().numpy() - ref) <= np.abs(ref) * (4 * 2.0 ** -24 + (2.0 ** -8 if grad == B.DQ_BF16 else 0.0))).all()
     assert ctx.dq_device_flags() == 0
+
+
+# ----------------------------------------------------------------------------------- product
+def spread_matrices(M, N, K, fa, fb, seed, together, every):
+    """Matrices whose scales run over the whole range, block by block of the reduction, while those of A and B together stay near `together`: all
+    products are ordinary numbers.  `every`: only each so many blocks of the reduction leave the middle."""
+    _, A, As = random_matrix(M, K, fa, seed)
+    _, Bm, Bs = random_matrix(N, K, fb, seed + 1)
+    nb, g = mx.blocks(K), rng(seed + 2)
+    lo, hi = -127 + max(together, 0), 127 + min(together, 0)
+    to_a = g.integers(lo, hi + 1, nb)
+    to_a[:2] = lo, hi
+    if every > 1:
+        to_a[np.arange(nb) % every != every - 1] = together // 2
+    out = []
+    for rows, fmt, codes, scales, mid in ((M, fa, A, As, to_a), (N, fb, Bm, Bs, together - to_a)):
+        byte = np.clip(mid[None, :] + 127 + g.integers(-2, 3, (rows, nb)), 0, 254).astype(np.uint8)
+        cb = B.dq_mx_row_bytes(fmt, K)[0]
+        if rows > 3:                                            # blocks of zeros, under scales of both ends
+            codes[rows // 2, :cb] = 0
+            byte[rows // 2, 0::2], byte[rows // 2, 1::2] = 0, 254
+        scales[:, :nb] = torch.from_numpy(byte)
+        out.append(mx.values(mx.unpack(codes[:, :cb].cpu().numpy(), fmt), byte, K, fmt))
+    return out[0], A, As, out[1], Bm, Bs
+
+
+# one for every kernel that the sizes choose (the last two: 256 x 256 tiles, 32 columns a workgroup)
+@pytest.mark.parametrize("M,N", [(5, 40), (30, 41), (24, 700), (100, 1503), (300, 280), (400, 701), (1000, 1601), (1701, 1750), (3601, 3570), (3, 8209)])
+@pytest.mark.parametrize("K", [70, 1700])
+@pytest.mark.parametrize("together,every", [(0, 1), (-100, 1), (90, 1), (0, 7)])
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_gemm_of_any_scales(ctx, fa, fb, cdt, together, every, K, M, N):
+    a, A, As, b, Bm, Bs = spread_matrices(M, N, K, fa, fb, 7 * M + K, together, every)
+    C = torch.full((M, up(N, 8)), float("nan"), dtype=TYPES[cdt], device="cuda")[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, C, cdt)
+    if M * N > 100000:                     # only the reference and its bound are formed by a library: fp64, on the GPU
+        ad, bd = torch.from_numpy(a).cuda(), torch.from_numpy(b).cuda().t().contiguous()
+        ref, s = (ad @ bd).cpu().numpy(), (ad.abs() @ bd.abs()).cpu().numpy()
+    else:
+        ref, s = a @ b.T, np.abs(a) @ np.abs(b).T
+    tol = s * (4 * -(-K // 128) + 16) * 2.0 ** -23                      # as product_bound
+    if cdt == B.DQ_BF16:
+        tol += np.abs(ref) * 2.0 ** -8 + (s * 2.0 ** -11 if B.DQ_MXFP8 in (fa, fb) else 0.0)
+    got = C.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert (np.abs(got - ref) <= tol + 1e-38).all()
+    again = torch.empty((M, up(N, 8)), dtype=TYPES[cdt], device="cuda")[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, again, cdt)
+    assert torch.equal(C, again)
+
+
+@pytest.mark.parametrize("M,N", [(5, 400), (30, 300), (24, 700), (100, 1503), (300, 400), (400, 701), (1000, 1601), (1701, 1750)])
+@pytest.mark.parametrize("fa,fb", [(1, 0), (0, 1), (1, 1)])
+def test_gemm_of_large_scales_is_as_near_as_of_small_ones(ctx, fa, fb, M, N):
+    """Normal values, A's times 2^60 and B's times 2^-60: 32 steps of 64, each eight sums.  256 roundings of at most 2^-24 of C's norm, of independent signs,
+    add up to 16 of them; summed to 14 bits eight at a time they would be off by 4e-6 (8 x 4 bits) to 1.5e-5 (8 x 8)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M)
+    K, parts, vals = 2048, [], []
+    for rows, fmt, factor in ((M, fa, 2.0 ** 60), (N, fb, 2.0 ** -60)):
+        X = torch.randn((rows, K), device="cuda", generator=g) * factor
+        c, s = stored(rows, K, fmt)
+        ctx.dq_mx_quantize(X, B.DQ_F32, fmt, c, s)
+        Y = torch.empty_like(X)
+        ctx.dq_mx_dequantize(fmt, c, s, Y, B.DQ_F32)
+        parts.append((c, s))
+        vals.append(Y.double())
+    ref = vals[0] @ vals[1].t().contiguous()
+    C = torch.empty((M, up(N, 4)), device="cuda")[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, *parts[0], fb, *parts[1], C, B.DQ_F32)
+    assert float(torch.linalg.norm(C.double() - ref)) <= 2e-6 * float(torch.linalg.norm(ref))
