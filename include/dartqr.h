@@ -371,8 +371,11 @@ dq_status dq_mx_rms_norm(dq_ctx* ctx, int T, int n, const void* X, dq_dtype xdt,
 
 /* C (M x N, fp32 or bf16) = A B^T for MX matrices A (M x K, a token a row) and B (N x K, an output channel a row), each of its own format: the
  * product of a linear layer.  fp32 accumulation, one rounding to a bf16 C.  With a bf16 C, products of 8-bit codes run on the matrix cores'
- * 8-bit path, which sums eight products at a time to about 14 bits (an error below 1e-4 of C's norm, against the 2^-9 of its own rounding); with an
- * fp32 C they are summed in fp32, for any scales (parts of C that meet scales of 2^17 and more, 255 apart, take six times as long).  A block whose scale is 255 makes its row of C (A) or column (B) NaN.
+ * 8-bit path, which sums eight products at a time to about 14 bits below the largest of them: before its rounding an element is off by at most 2^-11 of
+ * the sum of the magnitudes |a||b| that it is made of.  For normal values that comes to less than 1e-4 of C's norm, where the rounding makes 1.7e-3; where
+ * large products cancel it can exceed the rounding, and an fp32 C is the remedy: with one, products are summed in fp32, for any scales (parts of C that
+ * meet scales of 2^17 and more, 255 apart, take six times as long with an 8-bit operand).  A block whose scale is 255 makes its row of C (A) or column
+ * (B) NaN.
  * M = 0 or N = 0 is a no-op; K >= 1; M and N up to 2^26, K up to 2^31 - 1024 (DQ_ERR_UNSUPPORTED).  No workspace; a call gives the same bits every time. */
 dq_status dq_gemm_mx(dq_ctx* ctx, int M, int N, int K, dq_mx_format fa, const void* A, long lda,
                      const void* A_scales, long ldas, dq_mx_format fb, const void* B, long ldb,

@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 from oracle import mx_oracle as mx  # noqa: E402
 from paper_2511_04063_amd import binding as B  # noqa: E402
-from test_gpu_mx import TYPES, random_matrix, rng, stored, up  # noqa: E402
+from test_gpu_mx import TYPES, product_bound, random_matrix, rng, stored, up  # noqa: E402
 
 PAIRS = [(0, 0), (1, 0), (0, 1), (1, 1)]
 
@@ -123,3 +123,55 @@ def test_gemm_of_large_scales_is_as_near_as_of_small_ones(ctx, fa, fb, M, N):
     C = torch.empty((M, up(N, 4)), device="cuda")[:, :N]
     ctx.dq_gemm_mx(M, N, K, fa, *parts[0], fb, *parts[1], C, B.DQ_F32)
     assert float(torch.linalg.norm(C.double() - ref)) <= 2e-6 * float(torch.linalg.norm(ref))
+
+
+@pytest.mark.parametrize("M,N,K", [(8, 4000, 2048), (30, 1000, 2048), (300, 400, 2048), (300, 400, 16384), (2300, 2100, 1024), (3600, 3500, 512)])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_gemm_of_normal_values_before_the_rounding_to_bf16(ctx, fa, fb, M, N, K):
+    """How far a bf16 result is off before its rounding, from the elements that it rounds otherwise than the exact product does.  Where two values e apart
+    lie in cells of u, they are rounded apart, by u, with a chance of e / u; so the squared distance D^2 of the two rounded results comes to
+    sum |e| u <= ||e|| ||u|| <= 1e-4 ||C|| 2^-7 ||C|| where e is within the documented 1e-4 of C's norm (u <= 2^-7 |c|).  Counts of some hundred and more such
+    elements: a fifth more for their scatter.  For 4 x 4 bits, whose sums are fp32, 1e-5 is allowed in place of 1e-4."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M + K)
+    parts, vals = [], []
+    for rows, fmt in ((M, fa), (N, fb)):
+        X = torch.randn((rows, K), device="cuda", generator=g)
+        c, s = stored(rows, K, fmt)
+        ctx.dq_mx_quantize(X, B.DQ_F32, fmt, c, s)
+        Y = torch.empty_like(X)
+        ctx.dq_mx_dequantize(fmt, c, s, Y, B.DQ_F32)
+        parts.append((c, s))
+        vals.append(Y.double())
+    ref = vals[0] @ vals[1].t().contiguous()
+    H = torch.empty((M, up(N, 8)), device="cuda", dtype=torch.bfloat16)[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, *parts[0], fb, *parts[1], H, B.DQ_BF16)
+    apart = H.double() - ref.bfloat16().double()
+    norm = float(torch.linalg.norm(ref))
+    bound = (1e-4 if B.DQ_MXFP8 in (fa, fb) else 1e-5) * 2.0 ** -7 * 1.2
+    assert float(torch.linalg.norm(apart)) ** 2 <= bound * norm ** 2
+
+
+@pytest.mark.parametrize("M,N", [(8, 400), (30, 1000), (300, 400), (2300, 2100)])
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_gemm_whose_large_products_cancel(ctx, fa, fb, cdt, M, N):
+    """A channel that stands far above the others meets weights that cancel it: the documented bound goes with the sum of magnitudes, not with C."""
+    K = 1024
+    g = rng(M)
+    a, b = g.standard_normal((M, K)), g.standard_normal((N, K))
+    a[:, 0::64], b[:, 1::64] = 300.0, -b[:, 0::64]
+    a[:, 1::64] = a[:, 0::64]
+    parts, vals = [], []
+    for rows, fmt, x in ((M, fa, a), (N, fb, b)):
+        c, s = stored(rows, K, fmt)
+        ctx.dq_mx_quantize(torch.from_numpy(x).float().cuda(), B.DQ_F32, fmt, c, s)
+        Y = torch.empty((rows, K), device="cuda")
+        ctx.dq_mx_dequantize(fmt, c, s, Y, B.DQ_F32)
+        parts.append((c, s))
+        vals.append(Y.double().cpu().numpy())
+    ref = vals[0] @ vals[1].T
+    C = torch.empty((M, up(N, 8)), device="cuda", dtype=TYPES[cdt])[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, *parts[0], fb, *parts[1], C, cdt)
+    got = C.double().cpu().numpy()
+    assert (np.abs(got - ref) <= product_bound(*vals, ref, K, fa, fb, cdt)).all()
