@@ -175,3 +175,70 @@ def test_gemm_whose_large_products_cancel(ctx, fa, fb, cdt, M, N):
     ctx.dq_gemm_mx(M, N, K, fa, *parts[0], fb, *parts[1], C, cdt)
     got = C.double().cpu().numpy()
     assert (np.abs(got - ref) <= product_bound(*vals, ref, K, fa, fb, cdt)).all()
+
+
+# up to 16 rows against 8192 columns and more: 32 columns a workgroup
+@pytest.mark.parametrize("M,N,K", [(1, 8200, 1000), (9, 8209, 545), (16, 9001, 4096), (3, 8193, 31)])
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_gemm_of_few_rows_and_many_columns(ctx, fa, fb, cdt, M, N, K):
+    a, A, As = random_matrix(M, K, fa, 5 * M + K)
+    b, Bm, Bs = random_matrix(N, K, fb, 3 * N + K)
+    buf, C = view(M, N, up(N, 8) + 8, TYPES[cdt], 7.0)
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, C, cdt)
+    ref = a @ b.T
+    assert (np.abs(C.double().cpu().numpy() - ref) <= product_bound(a, b, ref, K, fa, fb, cdt)).all()
+    assert (buf[:, N:] == 7.0).all()
+    As[M - 1, (K - 1) // 32] = 255                              # the last block, cut short
+    Bs[N - 2, 0] = 255
+    bad = torch.zeros((M, N), dtype=torch.bool, device="cuda")
+    bad[M - 1], bad[:, N - 2] = True, True
+    D = torch.empty_like(buf)[:, :N]
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, D, cdt)
+    assert torch.equal(torch.isnan(D), bad)
+    got = torch.where(bad, torch.from_numpy(ref).cuda(), D.double()).cpu().numpy()
+    assert (np.abs(got - ref) <= product_bound(a, b, ref, K, fa, fb, cdt)).all()
+
+
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_gemm_of_rows_far_apart_and_many_columns(ctx, fa, fb, cdt):
+    """Rows of A, then of B, 8 MiB apart and more: B's last one starts 64 GiB behind the first."""
+    M, N, K, far = 37, 8209, 700, (1 << 23) + 64
+    a, A, As = random_matrix(M, K, fa, 91)
+    b, Bm, Bs = random_matrix(N, K, fb, 92)
+    ref = a @ b.T
+    for spread in ("a", "b"):
+        src = A if spread == "a" else Bm
+        wide = torch.empty((src.shape[0], far), dtype=torch.uint8, device="cuda")[:, :src.shape[1]]
+        wide.copy_(src)
+        C = torch.empty((M, up(N, 8)), dtype=TYPES[cdt], device="cuda")[:, :N]
+        ctx.dq_gemm_mx(M, N, K, fa, wide if spread == "a" else A, As, fb, wide if spread == "b" else Bm, Bs, C, cdt)
+        assert (np.abs(C.double().cpu().numpy() - ref) <= product_bound(a, b, ref, K, fa, fb, cdt)).all()
+        del wide
+
+
+@pytest.mark.parametrize("cdt", [B.DQ_F32, B.DQ_BF16])
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("M", [9, 40, 300])
+def test_gemm_whose_last_rows_of_b_start_beyond_32_bits(ctx, M, fa, fb, cdt):
+    """The product of rows of B 64 KiB apart gives the bits of the same rows close together."""
+    N, K, far = 70001, 96, 65536
+    _, A, As = random_matrix(M, K, fa, 81)
+    _, Bm, Bs = random_matrix(N, K, fb, 82)
+    wide = torch.empty((N, far), dtype=torch.uint8, device="cuda")
+    wide[:, :Bm.shape[1]] = Bm
+    scales = wide[:, 32768:32768 + Bs.shape[1]]
+    scales.copy_(Bs)
+    C = [torch.empty((M, up(N, 8)), dtype=TYPES[cdt], device="cuda")[:, :N] for _ in range(2)]
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, Bm, Bs, C[0], cdt)
+    ctx.dq_gemm_mx(M, N, K, fa, A, As, fb, wide[:, :Bm.shape[1]], scales, C[1], cdt)
+    assert torch.equal(C[0], C[1])
+    vals = []
+    for rows, fmt, c, s in ((M, fa, A, As), (4001, fb, Bm[N - 4001:], Bs[N - 4001:])):
+        Y = torch.empty((rows, K), device="cuda")
+        ctx.dq_mx_dequantize(fmt, c, s, Y, B.DQ_F32)
+        vals.append(Y.double().cpu().numpy())
+    ref = vals[0] @ vals[1].T
+    got = C[1][:, N - 4001:].double().cpu().numpy()
+    assert (np.abs(got - ref) <= product_bound(vals[0], vals[1], ref, K, fa, fb, cdt)).all()
