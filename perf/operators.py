@@ -245,8 +245,8 @@ _kept = {}
 
 def _library():
     """A context with its status word's memory for each stream that passes run on: a context's calls go to the stream that was the current one
-    when it was made.  (The raw handle, since torch.cuda.current_stream() takes 2.6 us, half of a call.)"""
-    device = torch.cuda.current_device()
+    when it was made.  (Raw handles, since torch.cuda.current_stream() takes 2.6 us, half of a call.)"""
+    device = torch._C._cuda_getDevice()
     key = (device, torch._C._cuda_getCurrentRawStream(device))
     lib = _kept.get(key)
     if lib is None:
