@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 from oracle import mx_oracle as mx  # noqa: E402
 from paper_2511_04063_amd import binding as B  # noqa: E402
-from test_gpu_mx import TYPES, product_bound, random_matrix, rng, stored, up  # noqa: E402
+from test_gpu_mx import TYPES, product_bound, random_matrix, rng, stored, up, view  # noqa: E402
 
 PAIRS = [(0, 0), (1, 0), (0, 1), (1, 1)]
 
