@@ -279,10 +279,11 @@ hipError_t launch_direct(const GemmMx& g, hipStream_t s) {
 // whose place the parts of stage i + kStages take.
 // The fragments of a step of 64 are read during the step before it.  Scales come in pieces of 16 a row, for 512 of the reduction, the same way.
 //
-// What bounds it.  256 x 256 tiles: the matrix cores and their power.  8192^3 of 4 x 4 bits takes 288 us (3.8 PFLOP/s), of 8 x 8 407 (2.7; the
-// library's product of plain fp8 matrices 398): the matrix cores are busy 57 and 70 % of the cycles, and the clock falls from 2.4 to 1.73 and 1.85 GHz.
-// A step of 64 costs 550 cycles of 512 in the matrix cores, and a round of tiles 12 us around its steps: 33 MB of C, the first loads, the launch.
-// fp32 results of 8-bit operands: bf16 arithmetic, 8192^3 890 us (1.24 PFLOP/s; the library's bf16 product 1.30).  Few tiles: latency of the loads.
+// What bounds it.  256 x 256 tiles: the steps, at the clock that the matrix cores' power leaves.  8192^3 of 4 x 4 bits takes 250 to 260 us (4.3 PFLOP/s), of
+// 8 x 4 364 (3.0), of 8 x 8 388 (2.8; the library's product of plain fp8 matrices 398): the matrix cores are busy 58, 74 and 69 % of the cycles, and the
+// clock falls from 2.4 to 1.8 and 1.95 GHz.  4 x 4 bits, K from 1024 to 8192 in two and in four rounds of tiles, take 9 us once (launch, operands from HBM,
+// the last tiles' ends), 4.3 a round and 0.44 a step of 64, 800 to 860 cycles of which the matrix cores need 512: 56 of the 75 us of 8192 x 4096, K 4096 are steps.
+// fp32 results of 8-bit operands: bf16 arithmetic, 8192^3 870 us (1.26 PFLOP/s; the library's bf16 product 1.30).  Few tiles: latency of the loads.
 //
 // LDS holds rows of 64 or 128 bytes as they are in memory, 16-byte chunk c at place c ^ swizzle(row): eight lanes in a row read from
 // different banks, and so do sixteen (no conflicts are counted).
@@ -722,7 +723,8 @@ hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
 
 // Which kernel, by what each takes for C = M x N, K (us of the kernel alone, operands in the caches; 4 x 4 bits and bf16 unless said):
 //   straight from memory, 16 rows, against 64 x 32 tiles   1 x 4096, 4096: 4.0, 6.1;  1 x 4096, 16384: 8.2, 11.8;  16 x 4096, 8192 (8 x 8): 11.1, 12.3;
-//                                                   16 x 8192, 4096: 6.0, 6.3;  but 16 x 8192, 8192: 9.8, 8.8, and 1 x 8192, 8192 (8 x 8, fp32) 20.3, 16.4
+//                                                   16 x 8192, 4096: 6.0, 6.3;  but 16 x 8192, 8192: 9.3, 8.2, and 1 x 8192, 8192 (8 x 8) 15.6, 13.3
+//                                                   (one row of 8 x 4 bits against 8192 columns, K 8192, would gain by it: 8.3, 10.2)
 //   the same, 32 rows x 16 (256 workgroups at most)   17 x 1000, 2000 (8 x 4): 3.8, 5.7;  300 x 300, 300 (8 x 8, fp32): 3.9, 7.3;  24 x 4096, 4096 (8 x 4): 7.2,
 //                                                   7.4;  but 24 x 8192, 2048 (512): 7.9, 6.1, and 64 x 1000, 8192 (8 x 4): 12.5, 9.8
 //   the same, 32 rows x 32 (256 workgroups at most)   24 x 8192, 2048 (8 x 4): 5.5, 6.1;  512 x 512, 512 (8 x 8, fp32): 5.0, 7.4;  but 24 x 8192, 4096 (8 x
@@ -732,7 +734,9 @@ hipError_t launch_tile(const GemmMx& g, hipStream_t s) {
 //   128 x 64 tiles against 128 x 128                512 x 4096, 4096 (256 and 128 workgroups): 10.8, 12.3;  1024 x 4096, 4096: 19.3, 14.4
 //   128 x 128 tiles, all of LDS against half          operands not in the L2s: 1024 x 4096, 4096 (256 workgroups): 17.1, 22.1;  2048 x 4096, 4096 (512): 32.5, 29.3
 //   128 x 128 tiles against 256 x 256               2048 x 4096, 4096 (512 and 128 workgroups): 25.0, 29.0
-// that is, the largest tile that still gives most compute units a workgroup.  (256 x 128 tiles in between: 24.3 for the last, but 39.7 against 37.6 for
+// that is, the largest tile that still gives most compute units a workgroup, by results of up to 8192 columns.  Tiles are counted, whatever part of their rows
+// exists: 24 x 14336, 4096 (8 x 4) takes 11.5 us in tiles of 128 x 64, 24 x 28672, 8192 27.6 in 128 x 128 and 1 x 128256, 8192 167 in 256 x 256, where B at the
+// rate of a large copy takes 6, 24 and 105.  (256 x 128 tiles in between: 24.3 for the last, but 39.7 against 37.6 for
 // 2560 x 4096, and 46.6 against 40.8 for 4096 x 4096, 1024 in bf16 arithmetic.)  A kernel of no work takes 2 us, one of 64 in the reduction 4 to 5.
 template <int FA, int FB, class OUT>
 hipError_t launch_types(const GemmMx& g, hipStream_t s) {
@@ -740,15 +744,16 @@ hipError_t launch_types(const GemmMx& g, hipStream_t s) {
     const bool near_rows = g.lda < (1L << 23) && g.ldb < (1L << 23);       // the tiles address their rows by 32-bit offsets
     const auto tiles = [&](long tm, long tn) { return ((g.M + tm - 1) / tm) * ((g.N + tn - 1) / tn); };
     if (!near_rows || (g.M <= 16 && (g.K <= 4096 || tiles(16, 16) <= 256))) {
-        // 32 columns a workgroup as soon as that gives every compute unit one: 1 x 8192, K 8192 8.1 -> 7.7 us
+        // 32 columns a workgroup as soon as that gives every compute unit one: 16 x 8192, K 4096 6.4 -> 5.6 us, 8 x 8 bits 10.3 -> 8.6 (one row 4.8 and 4.9, 7.4 and
+        // 7.2; but one row against 14336 columns, 8 x 8 bits, 13.7 -> 14.6)
         return g.N >= 32 * 256 ? launch_direct<FA, FB, OUT, 1, 2>(g, s) : launch_direct<FA, FB, OUT, 1, 1>(g, s);
     }
     if (g.K <= 4096 && tiles(32, 16) <= 256) return launch_direct<FA, FB, OUT, 2, 1>(g, s);
     if (g.K <= 2560 && tiles(32, 32) <= 256) return launch_direct<FA, FB, OUT, 2, 2>(g, s);
     constexpr long most = 192;
     if (!exact && tiles(256, 256) >= most) {
-        // Eight wavefronts to a tile for 4 x 4 bits (8192^3: 324 us with four, 299), four for the others, whose fragments do not leave registers for two
-        // wavefronts a SIMD (8 x 8 bits: 429 us, 476 with eight).
+        // Eight wavefronts to a tile for 4 x 4 bits (8192^3, when it was chosen: 324 us with four, 299), four for the others, whose fragments do not leave registers
+        // for two wavefronts a SIMD (8 x 8 bits: 429 us, 476 with eight).
         if constexpr (FA == DQ_MXFP4 && FB == DQ_MXFP4) return launch_tile<FA, FB, OUT, 4, 2, 8, 1, 160>(g, s);
         else if constexpr (!exact) return launch_tile<FA, FB, OUT, 4, 4, 4, 1, 160>(g, s);
     }
